@@ -238,6 +238,124 @@ int hisa_block_sparse_tokens(const hisa_queries* queries, const hisa_keys* keys,
 int hisa_index_iou(const int32_t* a_idx, const int32_t* b_idx, int32_t T, int32_t k, float* iou,
                    void* stream);
 
+/* ------------------------------------------------------------------------------------------------
+ * Around the indexer: a paged key/value cache, what fills it, and the attention that reads it.
+ * ---------------------------------------------------------------------------------------------- */
+
+/*
+ * A cache of n_pages pages of `page` token rows each, H_kv heads of d elements per row.  Row (page p,
+ * offset o, head h) begins page_stride * p + token_stride * o + head_stride * h elements behind k and
+ * behind v (one set of strides for both, so [n_pages, page, H_kv, d], [n_pages, H_kv, page, d] and
+ * arrays that interleave keys and values all fit); its d elements are contiguous.  Slot p * page + o
+ * names a row of all heads.  Rows that no slot or table names are never touched.
+ */
+typedef struct {
+  void*          k;           /* first key row, of `dtype` (device)                                    */
+  void*          v;           /* first value row; NULL for a cache of keys alone (hisa_cache_append)   */
+  float*         k_scale;     /* [n_pages, page, H_kv] fp32, required iff dtype == FP8: row = scale*code */
+  float*         v_scale;     /* the same for the values                                               */
+  const int32_t* block_table; /* [n_seq, max_pages]: page of tokens j*page .. of sequence n (device)   */
+  const int32_t* seq_len;     /* [n_seq] tokens of each sequence, the new ones included (device)       */
+  int64_t        page_stride, token_stride, head_stride;   /* in elements                              */
+  int32_t        n_pages;
+  int32_t        page;
+  int32_t        n_seq;
+  int32_t        max_pages;
+  int32_t        H_kv;
+  int32_t        d;
+  int32_t        dtype;       /* hisa_dtype                                                            */
+} hisa_cache;
+
+/*
+ * Block tables and slot maps of a batch from the lengths of its requests.  Sequence n holds ctx_len[n]
+ * tokens and receives new_len[n] more (negative lengths count as 0); the new tokens of all sequences
+ * stand in `rows` token rows, sequence after sequence.  All arrays are device arrays.
+ *   block_table [n_seq, max_pages] in/out: the entries ceil(ctx_len/page) .. ceil((ctx_len+new_len)/page)
+ *               - 1 of each sequence are taken from free_pages, in the order of the sequences; every
+ *               other entry is left as it was
+ *   free_pages  [n_free] page ids; the first page_start[n_seq] of them are in use afterwards.  If that
+ *               number exceeds n_free, the entries beyond are written as -1 and their tokens get no slot
+ *   seq_len     [n_seq] out: ctx_len + new_len, at most max_pages * page
+ *   q_start     [n_seq + 1] out: first token row of each sequence, and their number (at most rows)
+ *   page_start  [n_seq + 1] out: how many free pages the sequences before took, and all of them
+ *   q_seq, q_pos [rows] out: sequence and position of each token row, as hisa_queries takes them; rows
+ *               behind the last token (a padded batch): 0 and -1, a query that sees nothing
+ *   slots       [rows] out: slot of each token row in the pages, -1: none (padding, no page left, or
+ *               beyond max_pages * page)
+ *   key_rows    [rows] out or NULL: q_seq * s_max + q_pos, the row of the token in a padded key array
+ *               [n_seq, s_max, d] as hisa_keys describes it (-1: padding, or a position >= s_max)
+ * Arrays must not overlap.  Limits: n_seq <= 65535, rows <= 4194304, n_seq * max_pages and max_pages *
+ * page below 2^31, n_seq * s_max below 2^31 (with key_rows).  Needs no workspace.
+ */
+int hisa_page_tables(const int32_t* ctx_len, const int32_t* new_len, int32_t n_seq, int32_t* block_table,
+                     int32_t max_pages, int32_t page, const int32_t* free_pages, int32_t n_free, int32_t rows,
+                     int32_t s_max, int32_t* seq_len, int32_t* q_start, int32_t* page_start, int32_t* q_seq,
+                     int32_t* q_pos, int32_t* slots, int32_t* key_rows, void* stream);
+
+/*
+ * Writes T new rows (0: nothing to do) into the cache: row t of k_new (and of v_new, unless both it and cache->v are NULL)
+ * goes to slot slots[t]; a slot outside [0, n_pages * page) is skipped.  k_new, v_new: H_kv heads of d
+ * contiguous elements per row, rows src_stride elements apart (>= H_kv * d), of src_dtype (F32 or
+ * BF16).  Converted to cache->dtype: F32 (from F32), BF16 (rounded to nearest even), or FP8_E4M3 with
+ * one scale per row and head: scale = largest finite |element| / 448 (1 for a row of zeros, never
+ * below 2^-126), code = e4m3fn(element / scale) to nearest even; an element that is not finite becomes
+ * the NaN code.  Slots must differ from each other: which of two rows a slot named twice holds (or
+ * which part of each) is unspecified.  The indexer's padded key array is a cache of n_seq pages of
+ * s_max rows with one head and no values, and hisa_page_tables gives its slots as key_rows.
+ * block_table and seq_len are not read (may be NULL).  d % 8 == 0, d <= 512, strides multiples of 8;
+ * n_pages * page below 2^31; k, v, k_new, v_new 16-byte aligned, src_stride a multiple of 8.
+ * Needs no workspace.
+ */
+int hisa_cache_append(const hisa_cache* cache, const int32_t* slots, const void* k_new, const void* v_new,
+                      int32_t src_dtype, int64_t src_stride, int32_t T, void* stream);
+
+/*
+ * Attention of new tokens over the paged cache: for every query t (one of `T` token rows) and head h,
+ * over the positions s that it sees, q_lo[t] <= s <= q_pos[t] and s < seq_len of its sequence,
+ *   out[t, h, :] = sum_s p_s v_s / sum_s p_s,  p_s = exp(scale * q_{t,h} . k_s),  lse[t, h] = log sum_s p_s,
+ * where k_s, v_s are the rows of KV head h / (H / H_kv).  Nothing at a position that a query does not
+ * see affects its result, infinities and NaN included.  A query that sees no key gives zeros and -inf.
+ *   queries     q [T, H, d], T, H, q_dtype; q_pos (NULL: the new tokens are the last q_start[n+1] -
+ *               q_start[n] positions of their sequence) and q_lo (NULL: 0) as everywhere.  A document
+ *               or sliding-window mask is a q_lo, a prefix that sees itself whole a q_pos beyond the
+ *               own position.  w, q_seq and q_pos0 are not read
+ *   q_start     [n_seq + 1] first token row of each sequence, ascending (device, in), as
+ *               hisa_page_tables writes it.  Rows before q_start[0] and from q_start[n_seq] on belong to
+ *               nobody: their out and lse are left as they were
+ *   out         [T, H, d] of q_dtype (device, out)
+ *   lse         [T, H] fp32 (device, out) or NULL
+ * A block_table entry outside [0, n_pages) holds no key that anybody sees.
+ * Supported: q BF16 with a BF16 or FP8_E4M3 cache, d in {64, 128}; q F32 with an F32 cache, d % 4 == 0,
+ * d <= 256.  H <= 256, H_kv divides H; page a power of two; k, v and q 16-byte aligned, strides times
+ * the element size multiples of 16 bytes; max_pages * page and n_pages * page below 2^31;
+ * scale positive and finite.
+ * Scores, the running maximum and sum and the output are held in fp32; the weights p_s are rounded to
+ * bf16 for the second product (bf16 and fp8 caches).  All sums have a fixed order: the same call gives
+ * the same bits.
+ * Workspace: hisa_attention_workspace_bytes(queries, cache, 0), which depends on shapes only.
+ */
+int hisa_paged_attention(const hisa_queries* queries, const hisa_cache* cache, const int32_t* q_start,
+                         float scale, void* out, float* lse, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * The same attention over a list of positions per query: what Sparse MLA's sparse attention does with
+ * the indexer's output.  Query t of sequence q_seq[t] (NULL: 0) attends to the positions topk_idx[t, :]
+ * (order does not matter; a position named twice counts twice), entries outside [0, seq_len) are
+ * skipped, so both hisa_token_refine_topk's lists and hisa_block_sparse_tokens' fit; a query whose
+ * sequence is outside [0, n_seq) sees nothing.  Whether a position is visible is the list's business:
+ * q_pos and q_lo are not read.
+ *   topk_idx    [T, k] int32 (device, in), k <= 65536
+ * Everything else, the workspace rule (hisa_attention_workspace_bytes(queries, cache, k)) included, as
+ * hisa_paged_attention.
+ */
+int hisa_sparse_attention(const hisa_queries* queries, const hisa_cache* cache, const int32_t* topk_idx,
+                          int32_t k, float scale, void* out, float* lse, void* ws, size_t ws_bytes,
+                          void* stream);
+
+/* Workspace in bytes for hisa_paged_attention (k == 0) or hisa_sparse_attention (k >= 1) at these
+ * shapes; 0 if none is needed or the shapes are invalid. */
+size_t hisa_attention_workspace_bytes(const hisa_queries* queries, const hisa_cache* cache, int32_t k);
+
 /*
  * Attainable-peak probes for benchmarks (measurement aids; nothing of the paper's method).
  * hisa_probe_copy: one streaming device-to-device copy of `bytes` (a multiple of 16; both pointers

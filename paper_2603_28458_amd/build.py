@@ -7,14 +7,16 @@ from __future__ import annotations
 import os
 import subprocess
 import sys
+import tempfile
+from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB_DIR = os.path.join(HERE, "lib")
 LIB_PATH = os.path.join(LIB_DIR, "libhisa.so")
-SOURCES = ["hisa_api.hip"]
+SOURCES = ["hisa_api.hip", "serving_api.hip"]
 FLAGS = [
-    "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",
+    "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
     # packed-fp32 instructions are kept out of the generated code on purpose
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
     "-Wall", "-Wno-unused-function",
@@ -24,14 +26,23 @@ FLAGS = [
 def build(verbose: bool = True) -> str:
     os.makedirs(LIB_DIR, exist_ok=True)
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
-    cmd = [hipcc, *FLAGS, *[os.path.join(CSRC, s) for s in SOURCES], "-o", LIB_PATH]
-    if verbose:
-        print(" ".join(cmd), flush=True)
-    res = subprocess.run(cmd, capture_output=True, text=True)
+    # the sources are compiled side by side, then linked
+    with tempfile.TemporaryDirectory(dir=LIB_DIR) as tmp:
+        objects = [os.path.join(tmp, s + ".o") for s in SOURCES]
+        cmds = [[hipcc, *FLAGS, "-c", os.path.join(CSRC, s), "-o", o] for s, o in zip(SOURCES, objects)]
+        if verbose:
+            for cmd in cmds:
+                print(" ".join(cmd), flush=True)
+        with ThreadPoolExecutor(len(cmds)) as pool:
+            results = list(pool.map(lambda cmd: subprocess.run(cmd, capture_output=True, text=True), cmds))
+        if all(r.returncode == 0 for r in results):
+            results.append(subprocess.run([hipcc, "--offload-arch=gfx950", "-fPIC", "-shared", *objects, "-o", LIB_PATH],
+                                          capture_output=True, text=True))
     # hipcc's host pass warns that it does not know the packed-fp32 feature: harmless
-    err = "\n".join(l for l in res.stderr.splitlines() if "packed-fp32-ops" not in l)
-    if res.returncode != 0:
-        raise RuntimeError(f"hipcc failed ({res.returncode}):\n{res.stdout}\n{err}")
+    err = "\n".join(l for r in results for l in r.stderr.splitlines() if "packed-fp32-ops" not in l)
+    for r in results:
+        if r.returncode != 0:
+            raise RuntimeError(f"hipcc failed ({r.returncode}):\n{r.stdout}\n{err}")
     if verbose and err.strip():
         print(err, file=sys.stderr)
     try:

@@ -1,0 +1,241 @@
+// Host side of the calls around the indexer (include/hisa.h): argument validation, workspace carving and kernel launches
+// of the paged cache's upkeep and of the attention that reads it.  Nothing here allocates or synchronises.
+#include "../../include/hisa.h"
+
+#include <hip/hip_runtime.h>
+
+#include <cmath>
+
+#include "api_common.h"
+#include "attention_kernels.h"
+#include "cache_kernels.h"
+
+using namespace hisa;
+
+namespace {
+
+constexpr int kMaxHeads = 256, kMaxList = 65536, kMaxAppendD = 512;
+
+inline int elem_bytes(int dtype) { return dtype == HISA_F32 ? 4 : dtype == HISA_BF16 ? 2 : 1; }
+inline bool overflows31(long a, long b) { return a * b >= (1L << 31); }   // (both below 2^31)
+
+// What the append and the attention ask of a cache alike.
+int check_cache(const hisa_cache* c, long align) {
+  if (!c || !c->k) return HISA_ERR_NULL;
+  if (c->dtype < HISA_F32 || c->dtype > HISA_FP8_E4M3) return HISA_ERR_DTYPE;
+  if (c->n_pages < 1 || c->page < 1 || c->H_kv < 1 || c->H_kv > kMaxHeads || c->d < 1) return HISA_ERR_SHAPE;
+  if (overflows31(c->n_pages, c->page)) return HISA_ERR_SHAPE;
+  if (c->page_stride < 0 || c->token_stride < 0 || c->head_stride < 0) return HISA_ERR_SHAPE;
+  if (c->dtype == HISA_FP8_E4M3 && (!c->k_scale || (c->v && !c->v_scale))) return HISA_ERR_NULL;
+  if (!aligned16(c->k) || (c->v && !aligned16(c->v))) return HISA_ERR_ALIGN;
+  if (c->page_stride % align || c->token_stride % align || c->head_stride % align) return HISA_ERR_ALIGN;
+  return HISA_OK;
+}
+
+int check_attention(const hisa_queries* q, const hisa_cache* c, int32_t k) {
+  if (!q || !q->q) return HISA_ERR_NULL;
+  if (q->T < 1 || q->T > kMaxT || q->H < 1 || q->H > kMaxHeads) return HISA_ERR_SHAPE;
+  if (!aligned16(q->q)) return HISA_ERR_ALIGN;
+  if (!c) return HISA_ERR_NULL;
+  int st = check_cache(c, 16 / (c->dtype >= HISA_F32 && c->dtype <= HISA_FP8_E4M3 ? elem_bytes(c->dtype) : 1));
+  if (st) return st;
+  if (!c->v || !c->block_table || !c->seq_len) return HISA_ERR_NULL;
+  if (c->n_seq < 1 || c->n_seq > kMaxSeq || c->max_pages < 1 || q->H % c->H_kv) return HISA_ERR_SHAPE;
+  if (c->page & (c->page - 1) || overflows31(c->max_pages, c->page)) return HISA_ERR_SHAPE;
+  if (k < 0 || k > kMaxList) return HISA_ERR_SHAPE;
+  if (q->q_dtype == HISA_F32 && c->dtype == HISA_F32) {
+    if (c->d < 4 || c->d % 4 || c->d > kPlainMaxD) return HISA_ERR_SHAPE;
+  } else if (q->q_dtype == HISA_BF16 && (c->dtype == HISA_BF16 || c->dtype == HISA_FP8_E4M3)) {
+    if (c->d != 64 && c->d != 128) return HISA_ERR_SHAPE;
+  } else {
+    return HISA_ERR_DTYPE;
+  }
+  return HISA_OK;
+}
+
+// How a call is cut into workgroups; the same answer for the workspace and for the launch.
+struct AttnPlan {
+  int splits;
+  size_t ws_bytes;
+};
+
+AttnPlan plan_attention(const hisa_queries* q, const hisa_cache* c, int32_t k) {
+  AttnPlan p;
+  const long keys = k ? k : (long)c->max_pages * c->page;
+  const int G = q->H / c->H_kv;
+  const long wgs = (long)q->T * c->H_kv * ((G + kPlainHeads - 1) / kPlainHeads);
+  long splits = wgs >= 1024 ? 1 : (1024 + wgs - 1) / wgs;
+  const long most = (keys + 511) / 512;
+  if (splits > most) splits = most;
+  p.splits = (int)splits;
+  p.ws_bytes = splits > 1 ? (size_t)splits * q->T * q->H * (c->d + 2) * 4 : 0;
+  return p;
+}
+
+AttnArgs attention_args(const hisa_queries* q, const hisa_cache* c, float scale, void* out, float* lse) {
+  AttnArgs a{};
+  a.q = q->q;
+  a.q_seq = q->q_seq;
+  a.q_pos = q->q_pos;
+  a.q_lo = q->q_lo;
+  a.k = c->k;
+  a.v = c->v;
+  a.k_scale = c->k_scale;
+  a.v_scale = c->v_scale;
+  a.table = c->block_table;
+  a.seq_len = c->seq_len;
+  a.out = out;
+  a.lse = lse;
+  a.page_stride = c->page_stride;
+  a.token_stride = c->token_stride;
+  a.head_stride = c->head_stride;
+  a.scale_log2 = scale * 1.44269504088896341f;
+  a.T = q->T;
+  a.H = q->H;
+  a.H_kv = c->H_kv;
+  a.G = q->H / c->H_kv;
+  a.d = c->d;
+  a.n_pages = c->n_pages;
+  a.page_shift = __builtin_ctz(c->page);
+  a.n_seq = c->n_seq;
+  a.max_pages = c->max_pages;
+  return a;
+}
+
+template <bool LIST>
+int launch_attention(AttnArgs a, int q_dtype, int kv_dtype, hipStream_t st) {
+  const int chunks = (a.G + kPlainHeads - 1) / kPlainHeads;
+  const long wgs = (long)a.T * a.H_kv * chunks * a.splits;
+  if (wgs > kMaxGrid) return HISA_ERR_SHAPE;
+  const dim3 grid((unsigned)wgs), block(256);
+  if (kv_dtype == HISA_F32)
+    hipLaunchKernelGGL((k_attn_plain<0, 0, LIST>), grid, block, 0, st, a);
+  else if (kv_dtype == HISA_BF16)
+    hipLaunchKernelGGL((k_attn_plain<1, 1, LIST>), grid, block, 0, st, a);
+  else
+    hipLaunchKernelGGL((k_attn_plain<1, 2, LIST>), grid, block, 0, st, a);
+  if (a.splits > 1) {
+    const dim3 jg((unsigned)(((long)a.T * a.H * (a.d / 4) + 255) / 256));
+    if (q_dtype == HISA_F32)
+      hipLaunchKernelGGL((k_attn_join<0, LIST>), jg, block, 0, st, a);
+    else
+      hipLaunchKernelGGL((k_attn_join<1, LIST>), jg, block, 0, st, a);
+  }
+  return launch_status();
+}
+
+int attention(const hisa_queries* q, const hisa_cache* c, const int32_t* q_start, const int32_t* list, int32_t k,
+              float scale, void* out, float* lse, void* ws, size_t ws_bytes, void* stream) {
+  const int st = check_attention(q, c, k);
+  if (st) return st;
+  if (!out || (k ? !list : !q_start)) return HISA_ERR_NULL;
+  if (!aligned16(out)) return HISA_ERR_ALIGN;
+  if (!(scale > 0.f) || !std::isfinite(scale)) return HISA_ERR_SHAPE;
+  const AttnPlan p = plan_attention(q, c, k);
+  if (p.ws_bytes && (!ws || ws_bytes < p.ws_bytes)) return HISA_ERR_WORKSPACE;
+  if (p.ws_bytes && !aligned16(ws)) return HISA_ERR_ALIGN;
+  AttnArgs a = attention_args(q, c, scale, out, lse);
+  a.q_start = q_start;
+  a.list = list;
+  a.n_list = k;
+  a.part = (float*)ws;
+  a.splits = p.splits;
+  hipStream_t s = (hipStream_t)stream;
+  return k ? launch_attention<true>(a, q->q_dtype, c->dtype, s) : launch_attention<false>(a, q->q_dtype, c->dtype, s);
+}
+
+template <int SDT>
+void launch_append(const AppendArgs& a, int dtype, dim3 grid, hipStream_t st) {
+  if constexpr (SDT == HISA_F32)
+    if (dtype == HISA_F32) {
+      hipLaunchKernelGGL((k_cache_append<SDT, 0>), grid, dim3(256), 0, st, a);
+      return;
+    }
+  if (dtype == HISA_BF16) hipLaunchKernelGGL((k_cache_append<SDT, 1>), grid, dim3(256), 0, st, a);
+  else hipLaunchKernelGGL((k_cache_append<SDT, 2>), grid, dim3(256), 0, st, a);
+}
+
+}  // namespace
+
+extern "C" {
+
+int hisa_page_tables(const int32_t* ctx_len, const int32_t* new_len, int32_t n_seq, int32_t* block_table,
+                     int32_t max_pages, int32_t page, const int32_t* free_pages, int32_t n_free, int32_t rows,
+                     int32_t s_max, int32_t* seq_len, int32_t* q_start, int32_t* page_start, int32_t* q_seq,
+                     int32_t* q_pos, int32_t* slots, int32_t* key_rows, void* stream) {
+  if (!ctx_len || !new_len || !block_table || !seq_len || !q_start || !page_start || !q_seq || !q_pos || !slots)
+    return HISA_ERR_NULL;
+  if (n_free > 0 && !free_pages) return HISA_ERR_NULL;
+  if (n_seq < 1 || n_seq > kMaxSeq || max_pages < 1 || page < 1 || n_free < 0 || rows < 1 || rows > kMaxT)
+    return HISA_ERR_SHAPE;
+  if (overflows31(n_seq, max_pages) || overflows31(max_pages, page)) return HISA_ERR_SHAPE;
+  if (key_rows && (s_max < 1 || overflows31(n_seq, s_max))) return HISA_ERR_SHAPE;
+  TableArgs a{ctx_len, new_len, free_pages, block_table, seq_len, q_start,   page_start, q_seq, q_pos,
+              slots,   key_rows, n_seq,     max_pages,   page,    n_free,    rows,       s_max};
+  hipStream_t st = (hipStream_t)stream;
+  if (n_seq <= kTableThreads) {
+    const unsigned wgs = (unsigned)((rows + kTableThreads - 1) / kTableThreads);
+    hipLaunchKernelGGL(k_page_tables, dim3(wgs), dim3(kTableThreads), 0, st, a);
+  } else {
+    hipLaunchKernelGGL(k_page_scan, dim3(1), dim3(kTableThreads), 0, st, a);
+    hipLaunchKernelGGL(k_page_rows, dim3((unsigned)((rows + 255) / 256)), dim3(256), 0, st, a);
+  }
+  return launch_status();
+}
+
+int hisa_cache_append(const hisa_cache* cache, const int32_t* slots, const void* k_new, const void* v_new,
+                      int32_t src_dtype, int64_t src_stride, int32_t T, void* stream) {
+  const int st = check_cache(cache, 8);
+  if (st) return st;
+  if (T == 0) return HISA_OK;
+  if (!slots || !k_new || (v_new != nullptr) != (cache->v != nullptr)) return HISA_ERR_NULL;
+  if (src_dtype != HISA_F32 && src_dtype != HISA_BF16) return HISA_ERR_DTYPE;
+  if (src_dtype == HISA_BF16 && cache->dtype == HISA_F32) return HISA_ERR_DTYPE;
+  if (T < 1 || T > kMaxT || cache->d % 8 || cache->d > kMaxAppendD) return HISA_ERR_SHAPE;
+  if (src_stride < (int64_t)cache->H_kv * cache->d || src_stride >= (1L << 31)) return HISA_ERR_SHAPE;
+  if (src_stride % 8 || !aligned16(k_new) || (v_new && !aligned16(v_new))) return HISA_ERR_ALIGN;
+  AppendArgs a{};
+  a.src[0] = k_new;
+  a.src[1] = v_new;
+  a.dst[0] = cache->k;
+  a.dst[1] = cache->v;
+  a.scale[0] = cache->k_scale;
+  a.scale[1] = cache->v_scale;
+  a.slots = slots;
+  a.src_stride = src_stride;
+  a.page_stride = cache->page_stride;
+  a.token_stride = cache->token_stride;
+  a.head_stride = cache->head_stride;
+  a.T = T;
+  a.R = cache->H_kv;
+  a.d = cache->d;
+  a.page = cache->page;
+  a.arrays = v_new ? 2 : 1;
+  a.lanes = 1;
+  while (a.lanes * 8 < a.d) a.lanes *= 2;
+  a.n_slots = (long)cache->n_pages * cache->page;
+  const long rows = (long)T * a.R * a.arrays, per = 256 / a.lanes, wgs = (rows + per - 1) / per;
+  if (wgs > kMaxGrid) return HISA_ERR_SHAPE;
+  if (src_dtype == HISA_F32) launch_append<0>(a, cache->dtype, dim3((unsigned)wgs), (hipStream_t)stream);
+  else launch_append<1>(a, cache->dtype, dim3((unsigned)wgs), (hipStream_t)stream);
+  return launch_status();
+}
+
+int hisa_paged_attention(const hisa_queries* queries, const hisa_cache* cache, const int32_t* q_start,
+                         float scale, void* out, float* lse, void* ws, size_t ws_bytes, void* stream) {
+  return attention(queries, cache, q_start, nullptr, 0, scale, out, lse, ws, ws_bytes, stream);
+}
+
+int hisa_sparse_attention(const hisa_queries* queries, const hisa_cache* cache, const int32_t* topk_idx,
+                          int32_t k, float scale, void* out, float* lse, void* ws, size_t ws_bytes,
+                          void* stream) {
+  if (k < 1) return HISA_ERR_SHAPE;
+  return attention(queries, cache, nullptr, topk_idx, k, scale, out, lse, ws, ws_bytes, stream);
+}
+
+size_t hisa_attention_workspace_bytes(const hisa_queries* queries, const hisa_cache* cache, int32_t k) {
+  if (check_attention(queries, cache, k)) return 0;
+  return plan_attention(queries, cache, k).ws_bytes;
+}
+
+}  // extern "C"

@@ -21,7 +21,8 @@ LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "lib", "libh
 EXPORTS = ["hisa_pool_blocks", "hisa_pool_append", "hisa_block_score_topk", "hisa_token_refine_topk",
            "hisa_block_sparse_tokens", "hisa_index_iou", "dsa_flat_indexer_topk", "hisa_workspace_bytes",
            "hisa_status_string", "hisa_version", "hisa_probe_copy", "hisa_probe_mfma", "hisa_probe_mfma_fp8", "hisa_probe_mfma_toggling", "hisa_indexer_topk", "hisa_pool_blocks_max",
-           "hisa_token_refine_topk_static"]
+           "hisa_token_refine_topk_static", "hisa_page_tables", "hisa_cache_append", "hisa_paged_attention",
+           "hisa_sparse_attention", "hisa_attention_workspace_bytes"]
 STATIC_SCRATCH_BYTES = 16 << 20
 
 
@@ -40,6 +41,14 @@ class _Queries(C.Structure):
     _fields_ = [("q", C.c_void_p), ("w", C.c_void_p), ("q_seq", C.c_void_p), ("q_pos", C.c_void_p),
                 ("q_lo", C.c_void_p), ("T", C.c_int32), ("H", C.c_int32), ("q_pos0", C.c_int32),
                 ("q_dtype", C.c_int32)]
+
+
+class _Cache(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("k_scale", C.c_void_p), ("v_scale", C.c_void_p),
+                ("block_table", C.c_void_p), ("seq_len", C.c_void_p), ("page_stride", C.c_int64),
+                ("token_stride", C.c_int64), ("head_stride", C.c_int64), ("n_pages", C.c_int32), ("page", C.c_int32),
+                ("n_seq", C.c_int32), ("max_pages", C.c_int32), ("H_kv", C.c_int32), ("d", C.c_int32),
+                ("dtype", C.c_int32)]
 
 
 _lib = None
@@ -90,6 +99,17 @@ def lib() -> C.CDLL:
         L.hisa_probe_mfma_fp8.restype = C.c_int
         L.hisa_probe_mfma_toggling.argtypes = [vp, i32, i32, C.POINTER(C.c_double), vp]
         L.hisa_probe_mfma_toggling.restype = C.c_int
+        L.hisa_page_tables.argtypes = [vp, vp, i32, vp, i32, i32, vp, i32, i32, i32, vp, vp, vp, vp, vp, vp, vp, vp]
+        L.hisa_page_tables.restype = C.c_int
+        L.hisa_cache_append.argtypes = [C.POINTER(_Cache), vp, vp, vp, i32, C.c_int64, i32, vp]
+        L.hisa_cache_append.restype = C.c_int
+        L.hisa_paged_attention.argtypes = [C.POINTER(_Queries), C.POINTER(_Cache), vp, C.c_float, vp, vp, vp, sz, vp]
+        L.hisa_paged_attention.restype = C.c_int
+        L.hisa_sparse_attention.argtypes = [C.POINTER(_Queries), C.POINTER(_Cache), vp, i32, C.c_float, vp, vp, vp, sz,
+                                            vp]
+        L.hisa_sparse_attention.restype = C.c_int
+        L.hisa_attention_workspace_bytes.argtypes = [C.POINTER(_Queries), C.POINTER(_Cache), i32]
+        L.hisa_attention_workspace_bytes.restype = sz
         L.hisa_status_string.argtypes = [C.c_int]
         L.hisa_status_string.restype = C.c_char_p
         L.hisa_version.argtypes = []
@@ -150,9 +170,9 @@ class Keys:
 @dataclass
 class Queries:
     """Indexing queries q [T, H, d] (float32 / bfloat16), gates w [T, H] float32, optional
-    q_seq / q_pos / q_lo [T] int32; all on the GPU."""
+    q_seq / q_pos / q_lo [T] int32; all on the GPU.  (The attention calls read no gates: w may be None there.)"""
     q: torch.Tensor
-    w: torch.Tensor
+    w: Optional[torch.Tensor]
     dtype: int
     q_seq: Optional[torch.Tensor] = None
     q_pos: Optional[torch.Tensor] = None
@@ -342,6 +362,252 @@ def hisa_indexer_topk(queries: Queries, keys: Keys, pooled: torch.Tensor, pooled
                                  _ptr(topk_idx), _ptr(topk_scores), _stream(stream))
     _check(st, "hisa_indexer_topk")
     return block_idx, topk_idx, topk_scores
+
+
+# ---------------------------------------------------------------- the paged cache and its attention
+def _on_gpu(t: torch.Tensor) -> bool:
+    return t.is_cuda
+
+
+def _need(t, name: str, dtypes, shape=None, device=None, contiguous: bool = True):
+    """A tensor that a kernel can take as it is: on the GPU (the same one as the others), of the type and shape that the
+    call goes by."""
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name}: a tensor is needed, got {type(t).__name__}")
+    if not _on_gpu(t):
+        raise ValueError(f"{name}: not on the GPU ({t.device})")
+    if device is not None and t.device != device:
+        raise ValueError(f"{name}: on {t.device}, the other tensors are on {device}")
+    if t.dtype not in dtypes:
+        raise ValueError(f"{name}: {t.dtype}, needed is {' or '.join(str(d) for d in dtypes)}")
+    if shape is not None and tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name}: shape {tuple(t.shape)}, needed is {tuple(shape)}")
+    if contiguous and not t.is_contiguous():
+        raise ValueError(f"{name}: not contiguous")
+    return t
+
+
+_I32 = (torch.int32,)
+_F32 = (torch.float32,)
+_STORED = {HISA_F32: (torch.float32,), HISA_BF16: (torch.bfloat16,),
+           HISA_FP8_E4M3: (torch.float8_e4m3fn, torch.uint8)}
+
+
+class _on:
+    """The GPU that the tensors live on as the current one while a call is enqueued (a no-op if it is already)."""
+
+    def __init__(self, device):
+        self.guard = torch.cuda.device(device) if device.index != torch.cuda.current_device() else None
+
+    def __enter__(self):
+        if self.guard is not None:
+            self.guard.__enter__()
+
+    def __exit__(self, *exc):
+        if self.guard is not None:
+            self.guard.__exit__(*exc)
+        return False
+
+
+@dataclass
+class Cache:
+    """A paged cache: k, v [n_pages, page, H_kv, d] (float32 / bfloat16 / uint8 or float8 codes; any strides that k and v
+    share, the last dimension contiguous, so a transposed [n_pages, H_kv, page, d] or a slice of an array that holds both
+    fits), k_scale / v_scale [n_pages, page, H_kv] float32 for fp8, block_table [n_seq, max_pages] and seq_len [n_seq]
+    int32; all on the GPU.  v None: keys alone, block_table and seq_len None: to append to only."""
+    k: torch.Tensor
+    v: Optional[torch.Tensor]
+    dtype: int
+    block_table: Optional[torch.Tensor] = None
+    seq_len: Optional[torch.Tensor] = None
+    k_scale: Optional[torch.Tensor] = None
+    v_scale: Optional[torch.Tensor] = None
+
+    def __post_init__(self):
+        if self.dtype not in _STORED:
+            raise ValueError(f"dtype: unknown code {self.dtype}")
+        if self.k.dim() != 4:
+            raise ValueError(f"k: shape {tuple(self.k.shape)}, needed is [n_pages, page, H_kv, d]")
+        dev = self.k.device
+        for name, t in (("k", self.k), ("v", self.v)):
+            if t is None:
+                continue
+            _need(t, name, _STORED[self.dtype], self.k.shape, dev, contiguous=False)
+            if t.stride(3) != 1 and t.shape[3] > 1:
+                raise ValueError(f"{name}: the last dimension is not contiguous")
+            if t.stride() != self.k.stride():
+                raise ValueError(f"v: strides {t.stride()}, those of k are {self.k.stride()}")
+        for name, t in (("k_scale", self.k_scale), ("v_scale", self.v_scale)):
+            if t is not None:
+                _need(t, name, _F32, self.k.shape[:3], dev)
+        if self.block_table is not None:
+            _need(self.block_table, "block_table", _I32, None, dev)
+            if self.block_table.dim() != 2:
+                raise ValueError("block_table: needed is [n_seq, max_pages]")
+        if self.seq_len is not None:
+            _need(self.seq_len, "seq_len", _I32, None if self.block_table is None else self.block_table.shape[:1], dev)
+
+    def c(self) -> _Cache:
+        n, page, H_kv, d = self.k.shape
+        s = self.k.stride()
+        n_seq, max_pages = (0, 0) if self.block_table is None else self.block_table.shape
+        return _Cache(self.k.data_ptr(), None if self.v is None else self.v.data_ptr(), _ptr(self.k_scale),
+                      _ptr(self.v_scale), _ptr(self.block_table), _ptr(self.seq_len), s[0], s[1], s[2], n, page, n_seq,
+                      max_pages, H_kv, d, self.dtype)
+
+
+@dataclass
+class PageTables:
+    """What hisa_page_tables writes: seq_len [n_seq], q_start and page_start [n_seq + 1], q_seq, q_pos, slots and (or
+    None) key_rows [rows], all int32."""
+    seq_len: torch.Tensor
+    q_start: torch.Tensor
+    page_start: torch.Tensor
+    q_seq: torch.Tensor
+    q_pos: torch.Tensor
+    slots: torch.Tensor
+    key_rows: Optional[torch.Tensor] = None
+
+    @property
+    def pages_used(self) -> torch.Tensor:
+        """[1]: how many of the free pages are in use now (more than there were: too few)."""
+        return self.page_start[-1:]
+
+    @staticmethod
+    def empty(n_seq: int, rows: int, device, key_rows: bool = False) -> "PageTables":
+        def new(n):
+            return torch.empty((n,), dtype=torch.int32, device=device)
+
+        return PageTables(new(n_seq), new(n_seq + 1), new(n_seq + 1), new(rows), new(rows), new(rows),
+                          new(rows) if key_rows else None)
+
+
+def hisa_page_tables(ctx_len: torch.Tensor, new_len: torch.Tensor, block_table: torch.Tensor, page: int,
+                     free_pages: torch.Tensor, rows: int, s_max: int = 0, out: Optional[PageTables] = None,
+                     stream=None) -> PageTables:
+    """Block tables (updated in place) and slot maps of a batch from its requests' lengths; s_max > 0: key_rows too, the
+    tokens' rows in a padded key array [n_seq, s_max, d]."""
+    dev = ctx_len.device
+    _need(ctx_len, "ctx_len", _I32)
+    n_seq = ctx_len.numel()
+    _need(ctx_len, "ctx_len", _I32, (n_seq,))
+    _need(new_len, "new_len", _I32, (n_seq,), dev)
+    _need(block_table, "block_table", _I32, None, dev)
+    _need(free_pages, "free_pages", _I32, (free_pages.numel(),), dev)
+    if block_table.dim() != 2 or block_table.shape[0] != n_seq:
+        raise ValueError(f"block_table: shape {tuple(block_table.shape)}, needed is [{n_seq}, max_pages]")
+    if out is None:
+        out = PageTables.empty(n_seq, max(rows, 1), dev, key_rows=s_max > 0)
+    else:
+        for name, t, n in (("seq_len", out.seq_len, n_seq), ("q_start", out.q_start, n_seq + 1),
+                           ("page_start", out.page_start, n_seq + 1), ("q_seq", out.q_seq, rows),
+                           ("q_pos", out.q_pos, rows), ("slots", out.slots, rows)):
+            _need(t, name, _I32, (n,), dev)
+        if out.key_rows is not None:
+            _need(out.key_rows, "key_rows", _I32, (rows,), dev)
+    with _on(dev):
+        st = lib().hisa_page_tables(_ptr(ctx_len), _ptr(new_len), n_seq, _ptr(block_table), block_table.shape[1], page,
+                                    _ptr(free_pages), free_pages.numel(), rows, s_max, _ptr(out.seq_len),
+                                    _ptr(out.q_start), _ptr(out.page_start), _ptr(out.q_seq), _ptr(out.q_pos),
+                                    _ptr(out.slots), _ptr(out.key_rows), _stream(stream))
+    _check(st, "hisa_page_tables")
+    return out
+
+
+def hisa_cache_append(cache: Cache, slots: torch.Tensor, k_new: torch.Tensor, v_new: Optional[torch.Tensor] = None,
+                      stream=None) -> None:
+    """Rows k_new (and v_new) [T, H_kv, d] into the slots [T] of the cache, converted to its type.  The rows of a token
+    are contiguous, tokens may lie further apart (a slice of a wider projection), keys and values alike."""
+    dev = cache.k.device
+    T = slots.numel()
+    _need(slots, "slots", _I32, (T,), dev)
+    H_kv, d = cache.k.shape[2:]
+    stride = k_new.stride(0) if k_new.dim() == 3 and T > 1 else H_kv * d
+    for name, t in (("k_new", k_new), ("v_new", v_new)):
+        if t is None:
+            continue
+        _need(t, name, (torch.float32, torch.bfloat16), (T, H_kv, d), dev, contiguous=False)
+        if t.dtype != k_new.dtype:
+            raise ValueError(f"v_new: {t.dtype}, k_new is {k_new.dtype}")
+        if T and not t[0].is_contiguous():
+            raise ValueError(f"{name}: the rows of a token are not contiguous")
+        if T > 1 and t.stride(0) != stride:
+            raise ValueError(f"v_new: tokens {t.stride(0)} elements apart, those of k_new {stride}")
+    cc = cache.c()
+    with _on(dev):
+        st = lib().hisa_cache_append(C.byref(cc), _ptr(slots), k_new.data_ptr(),
+                                     None if v_new is None else v_new.data_ptr(),
+                                     HISA_F32 if k_new.dtype == torch.float32 else HISA_BF16, stride, T, _stream(stream))
+    _check(st, "hisa_cache_append")
+
+
+def hisa_attention_workspace_bytes(queries: Queries, cache: Cache, k: int = 0) -> int:
+    """Workspace of hisa_paged_attention (k == 0) or hisa_sparse_attention (k positions per query)."""
+    qc, cc = queries.c(), cache.c()
+    return int(lib().hisa_attention_workspace_bytes(C.byref(qc), C.byref(cc), k))
+
+
+def _attention(name: str, queries: Queries, cache: Cache, index: torch.Tensor, k: int, scale, out, lse, want_lse, ws,
+               stream):
+    q = queries.q
+    dev = cache.k.device
+    _need(q, "q", (torch.float32,) if queries.dtype == HISA_F32 else (torch.bfloat16,), None, dev)
+    if q.dim() != 3 or q.shape[2] != cache.k.shape[3]:
+        raise ValueError(f"q: shape {tuple(q.shape)}, needed is [T, H, {cache.k.shape[3]}]")
+    T, H, d = q.shape
+    for what, t in (("q_seq", queries.q_seq), ("q_pos", queries.q_pos), ("q_lo", queries.q_lo)):
+        if t is not None:
+            _need(t, what, _I32, (T,), dev)
+    if out is None:
+        out = torch.empty_like(q)
+    else:
+        _need(out, "out", (q.dtype,), q.shape, dev)
+    if lse is not None:
+        _need(lse, "lse", _F32, (T, H), dev)
+    elif want_lse:
+        lse = torch.empty((T, H), dtype=torch.float32, device=dev)
+    qc, cc = queries.c(), cache.c()
+    if ws is None:
+        nbytes = int(lib().hisa_attention_workspace_bytes(C.byref(qc), C.byref(cc), k))
+        ws = torch.empty(nbytes, dtype=torch.uint8, device=dev) if nbytes else None
+    else:
+        _need(ws, "ws", (torch.uint8,), None, dev)
+    scale = d ** -0.5 if scale is None else float(scale)
+    size = 0 if ws is None else ws.numel()
+    with _on(dev):
+        if k:
+            st = lib().hisa_sparse_attention(C.byref(qc), C.byref(cc), _ptr(index), k, scale, _ptr(out), _ptr(lse),
+                                             _ptr(ws), size, _stream(stream))
+        else:
+            st = lib().hisa_paged_attention(C.byref(qc), C.byref(cc), _ptr(index), scale, _ptr(out), _ptr(lse), _ptr(ws),
+                                            size, _stream(stream))
+    _check(st, name)
+    return out, lse
+
+
+def hisa_paged_attention(queries: Queries, cache: Cache, q_start: torch.Tensor, scale: Optional[float] = None,
+                         out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None, want_lse: bool = False,
+                         ws: Optional[torch.Tensor] = None, stream=None):
+    """Attention of new tokens over the paged cache; scale: d ** -0.5 unless given.  Returns (out [T, H, d], lse [T, H]
+    or None)."""
+    if cache.block_table is None or cache.seq_len is None or cache.v is None:
+        raise ValueError("cache: values, block_table and seq_len are needed")
+    _need(q_start, "q_start", _I32, (cache.block_table.shape[0] + 1,), cache.k.device)
+    return _attention("hisa_paged_attention", queries, cache, q_start, 0, scale, out, lse, want_lse, ws, stream)
+
+
+def hisa_sparse_attention(queries: Queries, cache: Cache, topk_idx: torch.Tensor, scale: Optional[float] = None,
+                          out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None, want_lse: bool = False,
+                          ws: Optional[torch.Tensor] = None, stream=None):
+    """Attention over the positions topk_idx [T, k] of each query (entries outside the sequence, -1 among them, are
+    skipped).  Returns (out [T, H, d], lse [T, H] or None)."""
+    if cache.block_table is None or cache.seq_len is None or cache.v is None:
+        raise ValueError("cache: values, block_table and seq_len are needed")
+    _need(topk_idx, "topk_idx", _I32, None, cache.k.device)
+    if topk_idx.dim() != 2 or topk_idx.shape[0] != queries.T or topk_idx.shape[1] < 1:
+        raise ValueError(f"topk_idx: shape {tuple(topk_idx.shape)}, needed is [{queries.T}, k]")
+    return _attention("hisa_sparse_attention", queries, cache, topk_idx, topk_idx.shape[1], scale, out, lse, want_lse, ws,
+                      stream)
 
 
 def hisa_probe_copy(src: torch.Tensor, dst: torch.Tensor, stream=None) -> int:
