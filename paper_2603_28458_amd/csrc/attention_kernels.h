@@ -47,29 +47,8 @@ __device__ __forceinline__ int clamp_len(const AttnArgs& a, int n) {
   return len < 0 ? 0 : len < cap ? len : (int)cap;
 }
 
-// Slot of position s of sequence n (whose table row is given), or -1: its page is no page of the cache.
-__device__ __forceinline__ long slot_of(const AttnArgs& a, const int32_t* __restrict__ table_row, int s) {
-  const int id = table_row[s >> a.page_shift];
-  return (uint32_t)id < (uint32_t)a.n_pages ? ((long)id << a.page_shift) + (s & ((1 << a.page_shift) - 1)) : -1;
-}
-__device__ __forceinline__ long row_of_slot(const AttnArgs& a, long slot) {
-  return (slot >> a.page_shift) * a.page_stride + (slot & ((1 << a.page_shift) - 1)) * a.token_stride;
-}
-
-// Four elements at row + e, widened.
-template <int DT>
-__device__ __forceinline__ float4 load_four(const void* base, long at) {
-  if constexpr (DT == 0) {
-    return *reinterpret_cast<const float4*>((const float*)base + at);
-  } else if constexpr (DT == 1) {
-    const uint2 w = *reinterpret_cast<const uint2*>((const uint16_t*)base + at);
-    return make_float4(__uint_as_float(w.x << 16), __uint_as_float(w.x & 0xffff0000u), __uint_as_float(w.y << 16),
-                       __uint_as_float(w.y & 0xffff0000u));
-  } else {
-    const int w = *reinterpret_cast<const int*>((const uint8_t*)base + at);
-    const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8(w, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8(w, true);
-    return make_float4(lo[0], lo[1], hi[0], hi[1]);
-  }
+__device__ __forceinline__ float4 load_f32x4(const void* base, long at) {
+  return *reinterpret_cast<const float4*>((const float*)base + at);
 }
 
 // One result row (or its part): o already holds the sum of the weighted values.
@@ -84,11 +63,11 @@ __device__ __forceinline__ void store_four(const AttnArgs& a, long row, int e, f
   }
 }
 
-// The plain kernel: one query token, up to 8 heads of one KV head, one part of its keys per workgroup of 4 waves.  A
+// fp32 queries and rows: one query token, up to 8 heads of one KV head, one part of its keys per workgroup of 4 waves.  A
 // wave takes every fourth tile of 64 keys: a key per lane for the scores, then 4 output columns per lane for the values.
 constexpr int kPlainHeads = 8, kPlainMaxD = 256;
 
-template <int QDT, int KDT, bool LIST>
+template <bool LIST>
 static __global__ __launch_bounds__(256) void k_attn_plain(AttnArgs a) {
   __shared__ float qs[kPlainHeads][kPlainMaxD];
   __shared__ float ps[4][kPlainHeads][64];
@@ -131,7 +110,7 @@ static __global__ __launch_bounds__(256) void k_attn_plain(AttnArgs a) {
 
   for (int i = threadIdx.x; i < heads * (a.d / 4); i += 256) {
     const int g = i / (a.d / 4), e = i % (a.d / 4) * 4;
-    const float4 x = load_four<QDT>(a.q, ((long)t * a.H + h0 + g) * a.d + e);
+    const float4 x = load_f32x4(a.q, ((long)t * a.H + h0 + g) * a.d + e);
     qs[g][e] = x.x * a.scale_log2;
     qs[g][e + 1] = x.y * a.scale_log2;
     qs[g][e + 2] = x.z * a.scale_log2;
@@ -150,40 +129,34 @@ static __global__ __launch_bounds__(256) void k_attn_plain(AttnArgs a) {
   const bool mine = lane * 4 < a.d;
   for (long tile = (long)begin + wave * 64; tile < end; tile += 256) {
     const int c = (int)tile + lane;
-    long slot = -1;
+    long at = -1;                         // this lane's row, if the query sees it
     if (c < end) {
       const int s = LIST ? a.list[(long)t * a.n_list + c] : c;
-      if (s >= 0 && s < len) slot = slot_of(a, row, s);
+      const int page = s >= 0 && s < len ? row[s >> a.page_shift] : -1;
+      if ((uint32_t)page < (uint32_t)a.n_pages)
+        at = page * a.page_stride + (s & ((1 << a.page_shift) - 1)) * a.token_stride + hk * a.head_stride;
     }
-    const long at = slot < 0 ? 0 : row_of_slot(a, slot) + hk * a.head_stride;
     float x[kPlainHeads];
 #pragma unroll
     for (int g = 0; g < kPlainHeads; ++g) x[g] = 0.f;
-    float vs = 1.f;
-    if (slot >= 0) {
+    if (at >= 0) {
       for (int e = 0; e < a.d; e += 4) {
-        const float4 kk = load_four<KDT>(a.k, at + e);
+        const float4 kk = load_f32x4(a.k, at + e);
 #pragma unroll
         for (int g = 0; g < kPlainHeads; ++g)
           x[g] = __builtin_fmaf(qs[g][e], kk.x,
                  __builtin_fmaf(qs[g][e + 1], kk.y, __builtin_fmaf(qs[g][e + 2], kk.z, __builtin_fmaf(qs[g][e + 3], kk.w, x[g]))));
       }
-      if constexpr (KDT == 2) {
-        const float ks = a.k_scale[slot * a.H_kv + hk];
-        vs = a.v_scale[slot * a.H_kv + hk];
-#pragma unroll
-        for (int g = 0; g < kPlainHeads; ++g) x[g] *= ks;
-      }
     }
-    vrow[wave][lane] = slot < 0 ? -1 : at;
+    vrow[wave][lane] = at;
 #pragma unroll
     for (int g = 0; g < kPlainHeads; ++g) {
-      if (slot < 0) x[g] = neg_inf();
+      if (at < 0) x[g] = neg_inf();
       float top = x[g];
       for (int s = 1; s < 64; s <<= 1) top = fmaxf(top, __shfl_xor(top, s));
       const float mn = fmaxf(m[g], top);
       const float base = mn == neg_inf() ? 0.f : mn;
-      const float p = slot < 0 ? 0.f : __builtin_amdgcn_exp2f(x[g] - base);
+      const float p = at < 0 ? 0.f : __builtin_amdgcn_exp2f(x[g] - base);
       const float shrink = __builtin_amdgcn_exp2f(m[g] - base);
       float sum = p;
       for (int s = 1; s < 64; s <<= 1) sum += __shfl_xor(sum, s);
@@ -193,13 +166,13 @@ static __global__ __launch_bounds__(256) void k_attn_plain(AttnArgs a) {
       o[g].z *= shrink;
       o[g].w *= shrink;
       m[g] = mn;
-      ps[wave][g][lane] = p * vs;
+      ps[wave][g][lane] = p;
     }
     wave_lds_order();
     for (int j = 0; j < 64; ++j) {
       const long vat = vrow[wave][j];
       if (vat < 0 || !mine) continue;
-      const float4 vv = load_four<KDT>(a.v, vat + lane * 4);
+      const float4 vv = load_f32x4(a.v, vat + lane * 4);
 #pragma unroll
       for (int g = 0; g < kPlainHeads; ++g) {
         const float p = ps[wave][g][j];
@@ -247,10 +220,789 @@ static __global__ __launch_bounds__(256) void k_attn_plain(AttnArgs a) {
       }
     } else {
       const float inv = sum == 0.f ? 0.f : 1.f / sum;
-      store_four<QDT>(a, r, e, make_float4(s.x * inv, s.y * inv, s.z * inv, s.w * inv));
+      store_four<0>(a, r, e, make_float4(s.x * inv, s.y * inv, s.z * inv, s.w * inv));
       if (e == 0 && a.lse) a.lse[r] = sum == 0.f ? neg_inf() : (base + log2f(sum)) * 0.693147180559945309f;
     }
   }
+}
+
+// ------------------------------------------------------------------------------------------
+// Matrix-core path (bf16 queries, bf16 or fp8 rows, d = 64 or 128).  Everything is computed transposed, keys (then
+// columns of the output) along the rows of the 32x32x16 MFMA and query rows along its columns: S^T = K Q^T, O^T = V^T P^T.
+// A lane then holds 16 scores of ONE query row per 32 keys: the softmax needs one exchange between lanes l and l ^ 32 per
+// tile, the row's maximum, sum and rescaling are per-lane numbers, and the weights are the second product's B operand as
+// they stand (an MFMA takes the contraction index in any order as long as both operands use the same: slots 0..3 and 4..7
+// of lane half h are keys 16 kk + 4 h + 0..3 and 16 kk + 8 + 4 h + 0..3, which is how the accumulator holds them).
+// A query row is (token, head of the KV head's group), tokens outermost, so few tokens of a wide group fill a tile too.
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef short s16x8 __attribute__((ext_vector_type(8)));
+typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+
+// A tile of rows in LDS, bf16, D elements per row, in 16-byte chunks that are permuted inside each row so that the reads
+// below meet no bank twice: keys are read 16 bytes per row by 32 consecutive rows, values 32 bytes of 4 consecutive rows
+// per 16 lanes (the transposing read).
+template <int D>
+struct RowTile {
+  static constexpr int kChunks = D / 8;           // of a row
+  static constexpr int kRowBytes = D * 2;
+  __device__ static __forceinline__ int key_byte(int r, int c) {
+    return r * kRowBytes + ((c ^ (D == 128 ? r & 15 : (r >> 1) & 7)) << 4);
+  }
+  __device__ static __forceinline__ int value_byte(int r, int c) {
+    return r * kRowBytes + ((c ^ (D == 128 ? (r & 7) << 1 : ((r >> 1) & 3) << 1)) << 4);
+  }
+  // A operand of the scores: key rows r0 .. r0 + 31, contraction step kk.
+  __device__ static __forceinline__ bf16x8 key_operand(const unsigned char* tile, int r0, int kk) {
+    const int lane = lane_id(), r = r0 + (lane & 31);
+    return as_bf16x8(*reinterpret_cast<const uint4*>(tile + key_byte(r, 2 * kk + (lane >> 5))));
+  }
+  // A operand of the output: columns 32 dt .. + 31, keys r0 .. r0 + 15 in the order of the weights' operand.
+  __device__ static __forceinline__ bf16x8 value_operand(const unsigned char* tile, int r0, int dt) {
+    const int lane = lane_id(), i = lane & 15;
+    const int r = r0 + 4 * (lane >> 5) + (i >> 2), c = dt * 4 + ((lane >> 4) & 1) * 2 + ((i >> 1) & 1);
+    const unsigned char* p = tile + value_byte(r, c) + (i & 1) * 8;
+    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)p);
+    const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p + 8 * kRowBytes));
+    const s16x8 v = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+    return __builtin_bit_cast(bf16x8, v);
+  }
+};
+
+// 16 stored bytes of a row as they go into a tile: bf16 as they are, fp8 widened (exactly) into two chunks.
+template <int KDT>
+__device__ __forceinline__ uint4 widen_fp8(uint32_t lo, uint32_t hi) {
+  const uint2 a = fp8x4_to_bf16x4(lo), b = fp8x4_to_bf16x4(hi);
+  return make_uint4(a.x, a.y, b.x, b.y);
+}
+template <int D, int KDT, bool VALUES>
+__device__ __forceinline__ void store_chunk(unsigned char* tile, int r, int c, uint4 x) {
+  using R = RowTile<D>;
+  if constexpr (KDT == 2) {
+    const uint4 a = widen_fp8<KDT>(x.x, x.y), b = widen_fp8<KDT>(x.z, x.w);
+    *reinterpret_cast<uint4*>(tile + (VALUES ? R::value_byte(r, 2 * c) : R::key_byte(r, 2 * c))) = a;
+    *reinterpret_cast<uint4*>(tile + (VALUES ? R::value_byte(r, 2 * c + 1) : R::key_byte(r, 2 * c + 1))) = b;
+  } else {
+    *reinterpret_cast<uint4*>(tile + (VALUES ? R::value_byte(r, c) : R::key_byte(r, c))) = x;
+  }
+}
+
+__device__ __forceinline__ float max_halves(float x) {   // with lane ^ 32
+  const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1]));
+}
+__device__ __forceinline__ float add_halves(float x) {
+  const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __uint_as_float(sw[0]) + __uint_as_float(sw[1]);
+}
+
+// 32 query rows of a wave.
+template <int D>
+struct RowState {
+  bf16x8 q[D / 16];      // B operand of the scores: row lane % 32
+  f32x16 o[D / 32];      // O^T: column = row lane % 32, register i of tile dt = output column 32 dt + 8 (i/4) + 4 half + i%4
+  float m, l;            // running maximum (x = scale_log2 * score) and this lane half's share of the sum
+  int pos, lo;           // what the row sees
+
+  __device__ __forceinline__ void clear() {
+    m = neg_inf();
+    l = 0.f;
+#pragma unroll
+    for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) o[dt][i] = 0.f;
+  }
+  __device__ __forceinline__ void load_q(const uint16_t* __restrict__ row) {
+    const int half = lane_id() >> 5;
+#pragma unroll
+    for (int kk = 0; kk < D / 16; ++kk) q[kk] = as_bf16x8(*reinterpret_cast<const uint4*>(row + kk * 16 + half * 8));
+  }
+};
+
+// How far a row's maximum may grow before its sums are rescaled: weights stay below 2^8, far inside what fp32 sums and
+// bf16 weights (whose precision is relative) hold, and most tiles need no pass over the accumulators.
+constexpr float kSlack = 8.f;
+
+// Hides the scores of a block of 32 keys that begins at `base`: key r counts where bit r of `keys` is set and the row
+// sees it.
+template <int D>
+__device__ __forceinline__ void hide(const RowState<D>& st, f32x16& s, uint32_t keys, int base) {
+  const int half4 = 4 * (lane_id() >> 5);
+  const uint32_t mine = keys >> half4;
+  const int last = st.pos - base - half4, first = st.lo - base - half4;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    const int r = 8 * (i >> 2) + (i & 3);
+    if (!(mine >> r & 1u) || r > last || r < first) s[i] = neg_inf();
+  }
+}
+
+template <int NB>
+__device__ __forceinline__ void scale_scores(f32x16 (&s)[NB], const float* ks) {   // fp8: the rows' scales
+  const int half = lane_id() >> 5;
+#pragma unroll
+  for (int b = 0; b < NB; ++b)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const float4 f = *reinterpret_cast<const float4*>(ks + b * 32 + 8 * j + 4 * half);
+      s[b][4 * j] *= f.x;
+      s[b][4 * j + 1] *= f.y;
+      s[b][4 * j + 2] *= f.z;
+      s[b][4 * j + 3] *= f.w;
+    }
+}
+
+// Scores of NB blocks of 32 keys -> weights as B operands; updates m, l, o.  vs: scales of the value rows (fp8).
+template <int D, int KDT, int NB>
+__device__ __forceinline__ void softmax_tile(RowState<D>& st, const f32x16 (&s)[NB], bf16x8 (&p)[2 * NB], float c,
+                                             const float* vs) {
+  const int half = lane_id() >> 5;
+  float top = neg_inf();
+#pragma unroll
+  for (int b = 0; b < NB; ++b)
+#pragma unroll
+    for (int i = 0; i < 16; i += 2) top = fmaxf(top, fmaxf(s[b][i], s[b][i + 1]));
+  top = max_halves(top) * c;
+  if (__builtin_amdgcn_ballot_w64(top > st.m + kSlack)) {
+    const float mn = fmaxf(st.m, top);
+    const float f = __builtin_amdgcn_exp2f(st.m - (mn == neg_inf() ? 0.f : mn));
+    st.m = mn;
+    st.l *= f;
+#pragma unroll
+    for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) st.o[dt][i] *= f;
+  }
+  const float off = st.m == neg_inf() ? 0.f : -st.m;
+  float sum0 = 0.f, sum1 = 0.f;
+#pragma unroll
+  for (int b = 0; b < NB; ++b)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      float w[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) w[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][4 * j + e], c, off));
+      sum0 += w[0] + w[1];
+      sum1 += w[2] + w[3];
+      if constexpr (KDT == 2) {
+        const float4 f = *reinterpret_cast<const float4*>(vs + b * 32 + 8 * j + 4 * half);
+        w[0] *= f.x;
+        w[1] *= f.y;
+        w[2] *= f.z;
+        w[3] *= f.w;
+      }
+#pragma unroll
+      for (int e = 0; e < 4; ++e) p[2 * b + (j >> 1)][4 * (j & 1) + e] = (__bf16)w[e];
+    }
+  st.l += sum0 + sum1;
+}
+
+// O^T += V^T P^T over NB blocks of 32 keys.
+template <int D, int NB, int NQ>
+__device__ __forceinline__ void add_values(RowState<D> (&st)[NQ], const unsigned char* tile,
+                                           const bf16x8 (&p)[NQ][2 * NB]) {
+#pragma unroll
+  for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+    for (int kk = 0; kk < 2 * NB; ++kk) {
+      const bf16x8 v = RowTile<D>::value_operand(tile, 16 * kk, dt);
+#pragma unroll
+      for (int n = 0; n < NQ; ++n) st[n].o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, p[n][kk], st[n].o[dt], 0, 0, 0);
+    }
+}
+
+// A value (or, fp8, its row's scale) that is infinite or NaN must not reach the rows that do not see it, and 0 * inf
+// would.  Where some rows of a wave see less of a tile than others, the bits of its values are looked at as they are
+// stored; a tile that holds such a value (rare enough) goes through add_values_apart.
+template <int KDT>
+__device__ __forceinline__ uint32_t not_finite(uint4 x) {
+  const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+  uint32_t odd = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    odd |= KDT == 2 ? ((w[i] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u : ((w[i] & 0x7fff7fffu) + 0x00800080u) & 0x80008000u;
+  return odd;
+}
+
+// The product with zeros in the places of such values (what it gives a row that sees none of them does not depend on
+// them, to the last bit), then, one key at a time, the products of its infinities and NaN alone, added to the rows that
+// see the key.
+__device__ __forceinline__ uint32_t odd_halves(uint32_t w) {   // 0xffff over each bf16 that is inf or NaN
+  return ((((w & 0x7fff7fffu) + 0x00800080u) & 0x80008000u) >> 15) * 0xffffu;
+}
+template <int D, int NB, int NQ>
+__device__ __forceinline__ void add_values_apart(RowState<D> (&st)[NQ], const unsigned char* tile,
+                                                 bf16x8 (&p)[NQ][2 * NB], int base) {
+  const int half = lane_id() >> 5;
+#pragma unroll
+  for (int n = 0; n < NQ; ++n)
+#pragma unroll
+    for (int kk = 0; kk < 2 * NB; ++kk)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const int s = base + 16 * kk + 8 * (e >> 2) + 4 * half + (e & 3);
+        if (s < st[n].lo || s > st[n].pos) p[n][kk][e] = (__bf16)0.f;
+      }
+#pragma unroll
+  for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+    for (int kk = 0; kk < 2 * NB; ++kk) {
+      Pack128 v;
+      v.v = RowTile<D>::value_operand(tile, 16 * kk, dt);
+      v.u = make_uint4(v.u.x & ~odd_halves(v.u.x), v.u.y & ~odd_halves(v.u.y), v.u.z & ~odd_halves(v.u.z),
+                       v.u.w & ~odd_halves(v.u.w));
+#pragma unroll
+      for (int n = 0; n < NQ; ++n)
+        st[n].o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v.v, p[n][kk], st[n].o[dt], 0, 0, 0);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+#pragma unroll 1
+  for (int key = 0; key < 32 * NB; ++key) {
+    const int in = key & 15, kk = key >> 4;
+    // slot of the key: lane half (in / 4) % 2, element (in / 8) * 4 + in % 4
+    const bool mine = half == ((in >> 2) & 1);
+    const int slot = (in >> 3) * 4 + (in & 3);
+    uint32_t keep[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) keep[e] = mine && slot >> 1 == e ? 0xffffu << (16 * (slot & 1)) : 0u;
+#pragma unroll
+    for (int n = 0; n < NQ; ++n) {
+      Pack128 w;
+      w.v = p[n][0];
+#pragma unroll
+      for (int x = 1; x < 2 * NB; ++x)
+        if (kk == x) w.v = p[n][x];
+      w.u = make_uint4(w.u.x & keep[0], w.u.y & keep[1], w.u.z & keep[2], w.u.w & keep[3]);
+      const bool sees = base + key >= st[n].lo && base + key <= st[n].pos;
+#pragma unroll
+      for (int dt = 0; dt < D / 32; ++dt) {
+        Pack128 v;
+        v.v = RowTile<D>::value_operand(tile, 16 * kk, dt);
+        v.u = make_uint4(v.u.x & odd_halves(v.u.x) & keep[0], v.u.y & odd_halves(v.u.y) & keep[1],
+                         v.u.z & odd_halves(v.u.z) & keep[2], v.u.w & odd_halves(v.u.w) & keep[3]);
+        f32x16 one;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) one[i] = 0.f;
+        one = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v.v, w.v, one, 0, 0, 0);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) st[n].o[dt][i] += sees ? one[i] : 0.f;
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    }
+  }
+}
+
+template <int D, int NB, int NQ>
+__device__ __forceinline__ void score_tile(const RowState<D> (&st)[NQ], const unsigned char* tile, f32x16 (&s)[NQ][NB]) {
+#pragma unroll
+  for (int b = 0; b < NB; ++b) {
+#pragma unroll
+    for (int n = 0; n < NQ; ++n)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) s[n][b][i] = 0.f;
+#pragma unroll
+    for (int kk = 0; kk < D / 16; ++kk) {
+      const bf16x8 a = RowTile<D>::key_operand(tile, 32 * b, kk);
+#pragma unroll
+      for (int n = 0; n < NQ; ++n) s[n][b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, st[n].q[kk], s[n][b], 0, 0, 0);
+    }
+  }
+}
+
+// What a query token sees of sequence n (ranges): clamped to the sequence, so that nothing behind it is read.
+struct Seen {
+  int lo, pos;
+};
+__device__ __forceinline__ Seen seen_by(const AttnArgs& a, int n, int len, int t, int t_end) {
+  Seen s;
+  const int pos = a.q_pos ? a.q_pos[t] : a.seq_len[n] - t_end + t;
+  const int lo = a.q_lo ? a.q_lo[t] : 0;
+  s.pos = pos < len ? pos : len - 1;
+  s.lo = lo > 0 ? lo : 0;
+  return s;
+}
+__device__ __forceinline__ int wave_max_int(int x) {
+  return __builtin_amdgcn_readfirstlane((int)(wave_max((uint32_t)x ^ 0x80000000u) ^ 0x80000000u));
+}
+__device__ __forceinline__ int wave_min_int(int x) {
+  return __builtin_amdgcn_readfirstlane((int)(wave_min((uint32_t)x ^ 0x80000000u) ^ 0x80000000u));
+}
+
+// The row tile `unit` of rows_per tile rows: sequence and first row in it, or -1.  Tiles are numbered so that sequence n
+// begins at floor(q_start[n] * G / rows_per) + n: at most one number per sequence stays unused, and the grid needs T,
+// n_seq and G alone.
+struct RowUnit {
+  int n, t_begin, t_end;   // sequence and its token rows
+  long r0;                 // first row (token, head) of the tile, in the sequence
+};
+template <int ROWS>
+__device__ __forceinline__ RowUnit find_unit(const AttnArgs& a, int unit) {
+  int lo = 0, hi = a.n_seq;
+  const int lane = lane_id();
+  while (hi - lo > 1) {              // 64 candidates at a time
+    const int step = (hi - lo + 63) / 64;
+    const int n = lo + lane * step;
+    const bool le = n < hi && (long)a.q_start[n] * a.G / ROWS + n <= unit;
+    const uint64_t b = __builtin_amdgcn_ballot_w64(le);
+    const int last = b ? 63 - __builtin_clzll(b) : 0;
+    lo += last * step;
+    hi = lo + step < hi ? lo + step : hi;
+  }
+  RowUnit u;
+  u.n = lo;
+  u.t_begin = a.q_start[lo];
+  u.t_end = a.q_start[lo + 1];
+  u.r0 = (unit - ((long)u.t_begin * a.G / ROWS + lo)) * ROWS;
+  return u;
+}
+
+// One result row: 4 columns at e of (t, h) row r, sums with maximum m and weight sum l.
+template <bool PART>
+__device__ __forceinline__ void store_result(const AttnArgs& a, int split, long r, int D, int e, float4 o, float m, float l) {
+  if constexpr (PART) {
+    const long pr = (long)split * a.T * a.H + r;
+    *reinterpret_cast<float4*>(a.part + pr * D + e) = o;
+    if (e == 0) {
+      float* ml = a.part + (long)a.splits * a.T * a.H * D + pr * 2;
+      ml[0] = m;
+      ml[1] = l;
+    }
+  } else {
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    store_four<1>(a, r, e, make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv));
+    if (e == 0 && a.lse) a.lse[r] = l == 0.f ? neg_inf() : (m + log2f(l)) * 0.693147180559945309f;
+  }
+}
+
+// ---- few rows per sequence, or lists: keys split over the waves --------------------------------
+// A workgroup of 4 waves takes NQ * 32 query rows of one KV head and a part of their keys.  Every wave works alone on its
+// own tiles of 32 keys (every fourth): the next tile's rows are on their way into registers while the present one, in the
+// wave's own 32 * D * 4 bytes of LDS, is multiplied; the waves' results are joined at the end.  Bound by memory: 4 D bytes
+// (bf16) per key and KV head, whatever the number of rows.
+constexpr int kRowWaves = 4;
+
+template <int D, int KDT>
+struct RowGeom {
+  static constexpr int kCpr = D * (KDT == 2 ? 1 : 2) / 16;   // stored 16-byte chunks of a row
+  static constexpr int kRpi = 64 / kCpr;                     // rows per load instruction
+  static constexpr int kNi = 32 / kRpi;                      // load instructions per 32 rows
+  static constexpr int kTile = 32 * D * 2;                   // LDS bytes of 32 keys, or values
+  static constexpr int kWaveLds = 2 * kTile + (KDT == 2 ? 256 : 0);
+  static constexpr int kLds = kRowWaves * kWaveLds + kRowWaves * 32 * 8;
+};
+
+template <int D, int KDT, int NQ, bool LIST>
+static __global__ __launch_bounds__(256, NQ == 1 ? 2 : 1) void k_attn_rows(AttnArgs a) {
+  using Geo = RowGeom<D, KDT>;
+  extern __shared__ __align__(16) unsigned char lds[];
+  const int lane = lane_id(), wave = threadIdx.x >> 6, half = lane >> 5, col = lane & 31;
+  unsigned char* kt = lds + wave * Geo::kWaveLds;
+  unsigned char* vt = kt + Geo::kTile;
+  float* sc = reinterpret_cast<float*>(vt + Geo::kTile);                       // 32 key scales, 32 value scales
+  float* join = reinterpret_cast<float*>(lds + kRowWaves * Geo::kWaveLds);     // [wave][32][2]
+
+  long id = blockIdx.x;
+  const int hk = (int)(id % a.H_kv);
+  id /= a.H_kv;
+  const int split = (int)(id % a.splits);
+  const int unit = (int)(id / a.splits);
+  int n, t_begin, t_end, len;
+  long r0, rows;                          // the tile's first row and the number of rows there are
+  if constexpr (LIST) {
+    const int tiles = (a.G + 32 * NQ - 1) / (32 * NQ);
+    t_begin = unit / tiles;
+    t_end = t_begin + 1;
+    r0 = (unit - (long)t_begin * tiles) * 32 * NQ;
+    rows = a.G;
+    n = a.q_seq ? a.q_seq[t_begin] : 0;
+    const bool none = (uint32_t)n >= (uint32_t)a.n_seq;
+    n = none ? 0 : n;
+    len = none ? 0 : clamp_len(a, n);
+  } else {
+    const RowUnit u = find_unit<32 * NQ>(a, unit);
+    n = u.n;
+    t_begin = u.t_begin;
+    t_end = u.t_end;
+    r0 = u.r0;
+    rows = (long)(t_end - t_begin) * a.G;
+    if (r0 < 0 || r0 >= rows || t_begin < 0 || t_end > a.T) return;
+    len = clamp_len(a, n);
+  }
+  const int32_t* __restrict__ table = a.table + (long)n * a.max_pages;
+
+  // the rows of this lane's columns (rows beyond the last one repeat it and are not stored)
+  RowState<D> st[NQ];
+  int pos_min = 0x7fffffff, pos_max = -1, lo_min = 0x7fffffff, lo_max = 0;
+#pragma unroll
+  for (int q = 0; q < NQ; ++q) {
+    long r = r0 + q * 32 + col;
+    if (r >= rows) r = rows - 1;
+    const int t = t_begin + (int)(r / a.G), h = hk * a.G + (int)(r % a.G);
+    st[q].clear();
+    st[q].load_q((const uint16_t*)a.q + ((long)t * a.H + h) * D);
+    if constexpr (LIST) {
+      st[q].pos = 0x7fffffff;
+      st[q].lo = 0;
+    } else {
+      const Seen s = seen_by(a, n, len, t, t_end);
+      st[q].pos = s.pos;
+      st[q].lo = s.lo;
+      pos_min = s.pos < pos_min ? s.pos : pos_min;
+      pos_max = s.pos > pos_max ? s.pos : pos_max;
+      lo_min = s.lo < lo_min ? s.lo : lo_min;
+      lo_max = s.lo > lo_max ? s.lo : lo_max;
+    }
+  }
+  int begin, end;                         // tiles of 32 keys (list entries); range tiles begin at multiples of 32
+  bool differ = false;                    // whether some rows see what others do not
+  if constexpr (LIST) {
+    begin = 0;
+    end = len > 0 ? (a.n_list + 31) / 32 : 0;
+  } else {
+    pos_min = wave_min_int(pos_min);
+    pos_max = wave_max_int(pos_max);
+    lo_min = wave_min_int(lo_min);
+    lo_max = wave_max_int(lo_max);
+    differ = pos_min != pos_max || lo_min != lo_max;
+    begin = lo_min >> 5;
+    end = (pos_max + 32) >> 5;
+    if (end < begin) end = begin;
+  }
+  if (a.splits > 1) {
+    // parts of at least 8 tiles (two per wave); the last parts of a short sequence are empty
+    const long nt = end - begin;
+    const long parts = nt < 8L * a.splits ? (nt + 7) / 8 : a.splits;
+    const int b0 = begin;
+    if (split < parts) {
+      begin = b0 + (int)(nt * split / parts);
+      end = b0 + (int)(nt * (split + 1) / parts);
+    } else {
+      end = begin;
+    }
+  }
+
+  // page lookups run two tiles ahead of the rows, list entries three
+  auto position = [&](int tile) {         // of key `col` of a tile, or -1
+    if (tile >= end) return -1;
+    const int c = tile * 32 + col;
+    if constexpr (LIST) return c < a.n_list ? a.list[(long)t_begin * a.n_list + c] : -1;
+    else return c;
+  };
+  auto page_of = [&](int s) {
+    const bool ok = LIST ? s >= 0 && s < len : s >= lo_min && s <= pos_max;
+    return ok ? table[s >> a.page_shift] : -1;
+  };
+  const unsigned char* __restrict__ kbase = (const unsigned char*)a.k + hk * a.head_stride * (KDT == 2 ? 1 : 2);
+  const unsigned char* __restrict__ vbase = (const unsigned char*)a.v + hk * a.head_stride * (KDT == 2 ? 1 : 2);
+  uint4 kr[Geo::kNi], vr[Geo::kNi];
+  float scale = 0.f;
+  uint32_t valid = 0;                     // rows of the tile in registers that there are
+  auto request = [&](int s, int page) {
+    const bool ok = (uint32_t)page < (uint32_t)a.n_pages;
+    valid = (uint32_t)__builtin_amdgcn_ballot_w64(ok);
+    const int o = s & ((1 << a.page_shift) - 1);
+    const long row = ok ? (page * a.page_stride + o * a.token_stride) * (KDT == 2 ? 1 : 2) : -1;
+#pragma unroll
+    for (int i = 0; i < Geo::kNi; ++i) {
+      const int r = i * Geo::kRpi + lane / Geo::kCpr;
+      const uint32_t lo = __shfl((uint32_t)row, r), hi = __shfl((uint32_t)((uint64_t)row >> 32), r);
+      const long at = (long)((uint64_t)hi << 32 | lo);
+      kr[i] = vr[i] = make_uint4(0, 0, 0, 0);
+      if (at >= 0) {
+        kr[i] = *reinterpret_cast<const uint4*>(kbase + at + lane % Geo::kCpr * 16);
+        vr[i] = *reinterpret_cast<const uint4*>(vbase + at + lane % Geo::kCpr * 16);
+      }
+    }
+    if constexpr (KDT == 2) {
+      const long slot = ((long)page << a.page_shift) + o;
+      scale = ok ? (half ? a.v_scale : a.k_scale)[slot * a.H_kv + hk] : 0.f;
+    }
+  };
+
+  int tile = begin + wave;
+  int s1 = position(tile), s2 = position(tile + kRowWaves);
+  request(s1, page_of(s1));
+  int p2 = page_of(s2);
+  int s3 = position(tile + 2 * kRowWaves);
+  for (; tile < end; tile += kRowWaves) {
+    const uint32_t keys = valid;
+    bool apart = false;
+    if (!LIST && differ) {                // rows that nobody sees are zeros by now
+      uint32_t odd = KDT == 2 && half && __builtin_isfpclass(scale, 0x207) ? 1u : 0u;
+#pragma unroll
+      for (int i = 0; i < Geo::kNi; ++i) odd |= not_finite<KDT>(vr[i]);
+      apart = __builtin_amdgcn_ballot_w64(odd != 0) != 0;
+    }
+#pragma unroll
+    for (int i = 0; i < Geo::kNi; ++i) {
+      const int r = i * Geo::kRpi + lane / Geo::kCpr;
+      store_chunk<D, KDT, false>(kt, r, lane % Geo::kCpr, kr[i]);
+      store_chunk<D, KDT, true>(vt, r, lane % Geo::kCpr, vr[i]);
+    }
+    if constexpr (KDT == 2) sc[lane] = scale;
+    wave_lds_order();
+    request(s2, p2);
+    s2 = s3;
+    p2 = page_of(s2);
+    s3 = position(tile + 3 * kRowWaves);
+
+    f32x16 s[NQ][1];
+    bf16x8 p[NQ][2];
+    score_tile<D, 1, NQ>(st, kt, s);
+    if constexpr (KDT == 2) {
+#pragma unroll
+      for (int q = 0; q < NQ; ++q) scale_scores<1>(s[q], sc);
+    }
+    const int base = LIST ? 0 : tile * 32;
+    if (keys != 0xffffffffu || (!LIST && (base + 31 > pos_min || base < lo_max))) {
+#pragma unroll
+      for (int q = 0; q < NQ; ++q) hide(st[q], s[q][0], keys, base);
+    }
+#pragma unroll
+    for (int q = 0; q < NQ; ++q) softmax_tile<D, KDT, 1>(st[q], s[q], p[q], a.scale_log2, sc + 32);
+    if (!LIST && apart) add_values_apart<D, 1, NQ>(st, vt, p, base);
+    else add_values<D, 1, NQ>(st, vt, p);
+    wave_lds_order();
+  }
+
+  // the waves' shares of every row, joined 32 rows at a time
+  float* part = reinterpret_cast<float*>(lds);             // [wave][D][32]
+#pragma unroll
+  for (int q = 0; q < NQ; ++q) {
+    const float l = add_halves(st[q].l);
+    __syncthreads();
+    if (half == 0) {
+      join[(wave * 32 + col) * 2] = st[q].m;
+      join[(wave * 32 + col) * 2 + 1] = l;
+    }
+    __syncthreads();
+    float top = neg_inf();
+#pragma unroll
+    for (int w = 0; w < kRowWaves; ++w) top = fmaxf(top, join[(w * 32 + col) * 2]);
+    const float base = top == neg_inf() ? 0.f : top;
+    float sum = 0.f;
+#pragma unroll
+    for (int w = 0; w < kRowWaves; ++w)
+      sum = __builtin_fmaf(__builtin_amdgcn_exp2f(join[(w * 32 + col) * 2] - base), join[(w * 32 + col) * 2 + 1], sum);
+    const float f = __builtin_amdgcn_exp2f(st[q].m - base);
+#pragma unroll
+    for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+      for (int i = 0; i < 16; ++i)
+        part[(wave * D + dt * 32 + 8 * (i >> 2) + 4 * half + (i & 3)) * 32 + col] = st[q].o[dt][i] * f;
+    __syncthreads();
+    const long r = r0 + q * 32 + col;
+    if (r < rows) {
+      const long row = (long)(t_begin + (int)(r / a.G)) * a.H + hk * a.G + (int)(r % a.G);
+#pragma unroll
+      for (int j = 0; j < D / 32; ++j) {
+        const int e = ((threadIdx.x >> 5) * (D / 32) + j) * 4;
+        float x[4];
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          x[c] = 0.f;
+#pragma unroll
+          for (int w = 0; w < kRowWaves; ++w) x[c] += part[(w * D + e + c) * 32 + col];
+        }
+        const float4 o = make_float4(x[0], x[1], x[2], x[3]);
+        if (a.splits > 1) store_result<true>(a, split, row, D, e, o, top, sum);
+        else store_result<false>(a, split, row, D, e, o, top, sum);
+      }
+    }
+  }
+}
+
+// ---- many rows per sequence ----------------------------------------------------------------------
+// A workgroup of 8 waves takes 256 query rows of one KV head (32 per wave) and a part of their keys, in tiles of 64 keys
+// that all waves multiply from LDS: two buffers, one barrier per tile, the tile after next on its way into registers.
+// Bound by the matrix units (4 D flop per visible pair): 8 waves are two per SIMD, so that one's softmax runs under the
+// other's products.
+constexpr int kChunkWaves = 8, kChunkRows = 32 * kChunkWaves, kChunkKeys = 64;
+
+template <int D, int KDT>
+struct ChunkGeom {
+  static constexpr int kCpr = D * (KDT == 2 ? 1 : 2) / 16;
+  static constexpr int kPerThread = 2 * kChunkKeys * kCpr / 512;      // 16-byte chunks of keys and values per thread
+  static constexpr int kTile = kChunkKeys * D * 2;
+  static constexpr int kBuffer = 2 * kTile + (KDT == 2 ? 2 * kChunkKeys * 4 : 0);
+  static constexpr int kLds = 2 * kBuffer + 32;
+};
+
+template <int D, int KDT>
+static __global__ __launch_bounds__(512, 2) void k_attn_chunk(AttnArgs a) {
+  using Geo = ChunkGeom<D, KDT>;
+  extern __shared__ __align__(16) unsigned char lds[];
+  const int lane = lane_id(), wave = threadIdx.x >> 6, half = lane >> 5, col = lane & 31;
+
+  long id = blockIdx.x;
+  const int hk = (int)(id % a.H_kv);
+  id /= a.H_kv;
+  const int split = (int)(id % a.splits);
+  const RowUnit u = find_unit<kChunkRows>(a, (int)(id / a.splits));
+  const int n = u.n, t_begin = u.t_begin, t_end = u.t_end;
+  const long r0 = u.r0, rows = (long)(t_end - t_begin) * a.G;
+  if (r0 < 0 || r0 >= rows || t_begin < 0 || t_end > a.T) return;
+  const int len = clamp_len(a, n);
+  const int32_t* __restrict__ table = a.table + (long)n * a.max_pages;
+
+  // what the whole tile of rows sees, and what this wave's rows see
+  int wg_pos = -1, wg_lo = 0x7fffffff, wg_pos_min = 0x7fffffff, wg_lo_max = 0;
+  {
+    const long last = r0 + kChunkRows - 1 < rows - 1 ? r0 + kChunkRows - 1 : rows - 1;
+    for (int i = (int)(r0 / a.G) + lane; i <= (int)(last / a.G); i += 64) {
+      const Seen s = seen_by(a, n, len, t_begin + i, t_end);
+      wg_pos = s.pos > wg_pos ? s.pos : wg_pos;
+      wg_lo = s.lo < wg_lo ? s.lo : wg_lo;
+      wg_pos_min = s.pos < wg_pos_min ? s.pos : wg_pos_min;
+      wg_lo_max = s.lo > wg_lo_max ? s.lo : wg_lo_max;
+    }
+    wg_pos_min = wave_min_int(wg_pos_min);
+    wg_lo_max = wave_max_int(wg_lo_max);
+    wg_pos = wave_max_int(wg_pos);
+    wg_lo = wave_min_int(wg_lo);
+  }
+  RowState<D> st[1];
+  long r = r0 + wave * 32 + col;
+  const bool mine = r < rows;
+  const bool idle = r0 + wave * 32 >= rows;                  // no row of this wave is there
+  if (!mine) r = rows - 1;
+  const int t = t_begin + (int)(r / a.G), h = hk * a.G + (int)(r % a.G);
+  st[0].clear();
+  st[0].load_q((const uint16_t*)a.q + ((long)t * a.H + h) * D);
+  {
+    const Seen s = seen_by(a, n, len, t, t_end);
+    st[0].pos = s.pos;
+    st[0].lo = s.lo;
+  }
+  const int pos_min = wave_min_int(st[0].pos), pos_max = wave_max_int(st[0].pos);
+  const int lo_min = wave_min_int(st[0].lo), lo_max = wave_max_int(st[0].lo);
+
+  int begin = wg_lo / kChunkKeys, end = (wg_pos + kChunkKeys) / kChunkKeys;
+  if (wg_pos < 0 || end < begin) end = begin;
+  if (a.splits > 1) {
+    const long nt = end - begin;
+    const long parts = nt < 4L * a.splits ? (nt + 3) / 4 : a.splits;     // of at least 4 tiles
+    const int b0 = begin;
+    if (split < parts) {
+      begin = b0 + (int)(nt * split / parts);
+      end = b0 + (int)(nt * (split + 1) / parts);
+    } else {
+      end = begin;
+    }
+  }
+
+  // this thread's chunks of a tile: chunk x = i * 512 + thread, keys first, then values
+  constexpr int kHalf = kChunkKeys * Geo::kCpr;
+  constexpr int kBytes = KDT == 2 ? 1 : 2;
+  auto row_of = [&](int i) { return ((i * 512 + (int)threadIdx.x) % kHalf) / Geo::kCpr; };
+  auto is_value = [&](int i) { return i * 512 + (int)threadIdx.x >= kHalf; };
+  auto page_of = [&](int tile, int row) {
+    const int s = tile * kChunkKeys + row;
+    return tile < end && s >= wg_lo && s <= wg_pos ? table[s >> a.page_shift] : -1;
+  };
+  int pages[Geo::kPerThread];
+  int scale_page = -1, mask_page = -1;
+  uint64_t there = 0;                      // rows of the tile in registers that are there
+  uint4 x[Geo::kPerThread];
+  float scale = 0.f;
+  auto lookup = [&](int tile) {
+#pragma unroll
+    for (int i = 0; i < Geo::kPerThread; ++i) pages[i] = page_of(tile, row_of(i));
+    mask_page = page_of(tile, lane);
+    if constexpr (KDT == 2) scale_page = threadIdx.x < 2 * kChunkKeys ? page_of(tile, threadIdx.x % kChunkKeys) : -1;
+  };
+  auto request = [&](int tile) {
+    there = __builtin_amdgcn_ballot_w64((uint32_t)mask_page < (uint32_t)a.n_pages);
+#pragma unroll
+    for (int i = 0; i < Geo::kPerThread; ++i) {
+      const int s = tile * kChunkKeys + row_of(i);
+      x[i] = make_uint4(0, 0, 0, 0);
+      if ((uint32_t)pages[i] < (uint32_t)a.n_pages) {
+        const long at = pages[i] * a.page_stride + (s & ((1 << a.page_shift) - 1)) * a.token_stride + hk * a.head_stride;
+        const unsigned char* src = (const unsigned char*)(is_value(i) ? a.v : a.k) + at * kBytes;
+        x[i] = *reinterpret_cast<const uint4*>(src + threadIdx.x % Geo::kCpr * 16);
+      }
+    }
+    if constexpr (KDT == 2) {
+      const int s = tile * kChunkKeys + threadIdx.x % kChunkKeys;
+      scale = 0.f;
+      if ((uint32_t)scale_page < (uint32_t)a.n_pages) {
+        const long slot = ((long)scale_page << a.page_shift) + (s & ((1 << a.page_shift) - 1));
+        scale = (threadIdx.x < kChunkKeys ? a.k_scale : a.v_scale)[slot * a.H_kv + hk];
+      }
+    }
+  };
+  uint64_t* masks = reinterpret_cast<uint64_t*>(lds + 2 * Geo::kBuffer);     // of the two buffers
+  int* odd = reinterpret_cast<int*>(masks + 2);                               // tile with infinities or NaN that not
+  if (threadIdx.x < 2) odd[threadIdx.x] = -1;                                 // every row of the workgroup sees
+  __syncthreads();
+  auto deposit = [&](int buffer, int tile) {
+    unsigned char* kt = lds + buffer * Geo::kBuffer;
+    unsigned char* vt = kt + Geo::kTile;
+#pragma unroll
+    for (int i = 0; i < Geo::kPerThread; ++i) {
+      const int c = threadIdx.x % Geo::kCpr;
+      if (is_value(i)) store_chunk<D, KDT, true>(vt, row_of(i), c, x[i]);
+      else store_chunk<D, KDT, false>(kt, row_of(i), c, x[i]);
+    }
+    if constexpr (KDT == 2)
+      if (threadIdx.x < 2 * kChunkKeys) reinterpret_cast<float*>(vt + Geo::kTile)[threadIdx.x] = scale;
+    if (threadIdx.x == 0) masks[buffer] = there;
+    if (tile * kChunkKeys + kChunkKeys - 1 > wg_pos_min || tile * kChunkKeys < wg_lo_max) {
+      bool found = KDT == 2 && threadIdx.x >= kChunkKeys && __builtin_isfpclass(scale, 0x207);
+#pragma unroll
+      for (int i = 0; i < Geo::kPerThread; ++i) found |= is_value(i) && not_finite<KDT>(x[i]) != 0;
+      if (found) odd[buffer] = tile;
+    }
+  };
+
+  lookup(begin);
+  request(begin);
+  lookup(begin + 1);
+  deposit(0, begin);
+  request(begin + 1);
+  lookup(begin + 2);
+  __syncthreads();
+  for (int tile = begin; tile < end; ++tile) {
+    const int buffer = (tile - begin) & 1;
+    const unsigned char* kt = lds + buffer * Geo::kBuffer;
+    const unsigned char* vt = kt + Geo::kTile;
+    const float* sc = reinterpret_cast<const float*>(vt + Geo::kTile);
+    const int base = tile * kChunkKeys;
+    if (!idle && base <= pos_max && base + kChunkKeys - 1 >= lo_min) {
+      const uint64_t mask = masks[buffer];
+      const uint32_t keys[2] = {(uint32_t)mask, (uint32_t)(mask >> 32)};
+      f32x16 s[1][2];
+      bf16x8 p[1][4];
+      score_tile<D, 2, 1>(st, kt, s);
+      if constexpr (KDT == 2) scale_scores<2>(s[0], sc);
+      if ((keys[0] & keys[1]) != 0xffffffffu || base + kChunkKeys - 1 > pos_min || base < lo_max) {
+        hide(st[0], s[0][0], keys[0], base);
+        hide(st[0], s[0][1], keys[1], base + 32);
+      }
+      softmax_tile<D, KDT, 2>(st[0], s[0], p[0], a.scale_log2, sc + kChunkKeys);
+      if (odd[buffer] == tile) add_values_apart<D, 2, 1>(st, vt, p, base);
+      else add_values<D, 2, 1>(st, vt, p);
+    }
+    if (tile + 1 < end) {
+      deposit(buffer ^ 1, tile + 1);
+      request(tile + 2);
+      lookup(tile + 3);
+    }
+    __syncthreads();
+  }
+
+  if (!mine) return;
+  const float l = add_halves(st[0].l);
+  const long row = (long)t * a.H + h;
+#pragma unroll
+  for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int e = dt * 32 + 8 * j + 4 * half;
+      const float4 o = make_float4(st[0].o[dt][4 * j], st[0].o[dt][4 * j + 1], st[0].o[dt][4 * j + 2], st[0].o[dt][4 * j + 3]);
+      if (a.splits > 1) store_result<true>(a, split, row, D, e, o, st[0].m, l);
+      else store_result<false>(a, split, row, D, e, o, st[0].m, l);
+    }
 }
 
 // Joins the parts of a row: 4 columns per lane, rows of a token in consecutive groups of lanes.

@@ -54,21 +54,43 @@ int check_attention(const hisa_queries* q, const hisa_cache* c, int32_t k) {
 }
 
 // How a call is cut into workgroups; the same answer for the workspace and for the launch.
+enum AttnKernel { ATTN_PLAIN, ATTN_ROWS, ATTN_CHUNK };
 struct AttnPlan {
-  int splits;
+  AttnKernel kernel;
+  int row_tiles;      // ATTN_ROWS: 32 query rows each, per wave
+  long units;         // tiles of query rows, of one KV head
+  int splits;         // parts of their keys
   size_t ws_bytes;
 };
 
 AttnPlan plan_attention(const hisa_queries* q, const hisa_cache* c, int32_t k) {
-  AttnPlan p;
+  AttnPlan p{};
   const long keys = k ? k : (long)c->max_pages * c->page;
-  const int G = q->H / c->H_kv;
-  const long wgs = (long)q->T * c->H_kv * ((G + kPlainHeads - 1) / kPlainHeads);
-  long splits = wgs >= 1024 ? 1 : (1024 + wgs - 1) / wgs;
-  const long most = (keys + 511) / 512;
+  const long G = q->H / c->H_kv, T = q->T;
+  long most, want;
+  if (c->dtype == HISA_F32) {
+    p.kernel = ATTN_PLAIN;
+    p.units = T * ((G + kPlainHeads - 1) / kPlainHeads);
+    most = (keys + 511) / 512;
+    want = 1024;
+  } else if (k || T * G <= 64L * c->n_seq) {
+    p.kernel = ATTN_ROWS;
+    p.row_tiles = (k ? G > 32 : T * G > 32L * c->n_seq) ? 2 : 1;
+    const long rows = 32 * p.row_tiles;
+    p.units = k ? T * ((G + rows - 1) / rows) : T * G / rows + c->n_seq;
+    most = (keys + 255) / 256;
+    want = 2048;
+  } else {
+    p.kernel = ATTN_CHUNK;
+    p.units = T * G / kChunkRows + c->n_seq;
+    most = (keys + 255) / 256;
+    want = 256;
+  }
+  const long wgs = p.units * c->H_kv;
+  long splits = (want + wgs - 1) / wgs;
   if (splits > most) splits = most;
   p.splits = (int)splits;
-  p.ws_bytes = splits > 1 ? (size_t)splits * q->T * q->H * (c->d + 2) * 4 : 0;
+  p.ws_bytes = splits > 1 ? (size_t)splits * T * q->H * (c->d + 2) * 4 : 0;
   return p;
 }
 
@@ -102,24 +124,47 @@ AttnArgs attention_args(const hisa_queries* q, const hisa_cache* c, float scale,
   return a;
 }
 
+template <int D, int KDT, int NQ, bool LIST>
+int launch_rows(const AttnArgs& a, dim3 grid, hipStream_t st) {
+  constexpr auto kern = k_attn_rows<D, KDT, NQ, LIST>;
+  constexpr int lds = RowGeom<D, KDT>::kLds;
+  if (lds > 65536 && raise_lds_limit<kern>(lds)) return HISA_ERR_LAUNCH;
+  hipLaunchKernelGGL(kern, grid, dim3(64 * kRowWaves), lds, st, a);
+  return HISA_OK;
+}
+
+template <int D, int KDT, bool LIST>
+int launch_mfma(const AttnArgs& a, const AttnPlan& p, dim3 grid, hipStream_t st) {
+  if (p.kernel == ATTN_ROWS)
+    return p.row_tiles == 2 ? launch_rows<D, KDT, 2, LIST>(a, grid, st) : launch_rows<D, KDT, 1, LIST>(a, grid, st);
+  if constexpr (!LIST) {
+    constexpr auto kern = k_attn_chunk<D, KDT>;
+    constexpr int lds = ChunkGeom<D, KDT>::kLds;
+    if (lds > 65536 && raise_lds_limit<kern>(lds)) return HISA_ERR_LAUNCH;
+    hipLaunchKernelGGL(kern, grid, dim3(64 * kChunkWaves), lds, st, a);
+  }
+  return HISA_OK;
+}
+
 template <bool LIST>
-int launch_attention(AttnArgs a, int q_dtype, int kv_dtype, hipStream_t st) {
-  const int chunks = (a.G + kPlainHeads - 1) / kPlainHeads;
-  const long wgs = (long)a.T * a.H_kv * chunks * a.splits;
+int launch_attention(AttnArgs a, const AttnPlan& p, int dtype, hipStream_t st) {
+  const long wgs = p.units * a.H_kv * a.splits;
   if (wgs > kMaxGrid) return HISA_ERR_SHAPE;
-  const dim3 grid((unsigned)wgs), block(256);
-  if (kv_dtype == HISA_F32)
-    hipLaunchKernelGGL((k_attn_plain<0, 0, LIST>), grid, block, 0, st, a);
-  else if (kv_dtype == HISA_BF16)
-    hipLaunchKernelGGL((k_attn_plain<1, 1, LIST>), grid, block, 0, st, a);
+  const dim3 grid((unsigned)wgs);
+  int status = HISA_OK;
+  if (dtype == HISA_F32)
+    hipLaunchKernelGGL((k_attn_plain<LIST>), grid, dim3(256), 0, st, a);
+  else if (dtype == HISA_BF16)
+    status = a.d == 128 ? launch_mfma<128, 1, LIST>(a, p, grid, st) : launch_mfma<64, 1, LIST>(a, p, grid, st);
   else
-    hipLaunchKernelGGL((k_attn_plain<1, 2, LIST>), grid, block, 0, st, a);
+    status = a.d == 128 ? launch_mfma<128, 2, LIST>(a, p, grid, st) : launch_mfma<64, 2, LIST>(a, p, grid, st);
+  if (status) return status;
   if (a.splits > 1) {
     const dim3 jg((unsigned)(((long)a.T * a.H * (a.d / 4) + 255) / 256));
-    if (q_dtype == HISA_F32)
-      hipLaunchKernelGGL((k_attn_join<0, LIST>), jg, block, 0, st, a);
+    if (dtype == HISA_F32)
+      hipLaunchKernelGGL((k_attn_join<0, LIST>), jg, dim3(256), 0, st, a);
     else
-      hipLaunchKernelGGL((k_attn_join<1, LIST>), jg, block, 0, st, a);
+      hipLaunchKernelGGL((k_attn_join<1, LIST>), jg, dim3(256), 0, st, a);
   }
   return launch_status();
 }
@@ -141,7 +186,7 @@ int attention(const hisa_queries* q, const hisa_cache* c, const int32_t* q_start
   a.part = (float*)ws;
   a.splits = p.splits;
   hipStream_t s = (hipStream_t)stream;
-  return k ? launch_attention<true>(a, q->q_dtype, c->dtype, s) : launch_attention<false>(a, q->q_dtype, c->dtype, s);
+  return k ? launch_attention<true>(a, p, c->dtype, s) : launch_attention<false>(a, p, c->dtype, s);
 }
 
 template <int SDT>
