@@ -30,13 +30,17 @@ struct AttnArgs {
   int splits;
 };
 
-// Last n in [0, n_seq) with q_start[n] <= t; whether t is a row of it is the caller's to check.
-__device__ __forceinline__ int seq_of_row(const int32_t* __restrict__ q_start, int n_seq, int t) {
+// Last n in [0, n_seq) for which `le(n)` holds (ascending: true up to it), by the whole wave, 64 candidates at a time; 0 if
+// it holds for none.
+template <class Le>
+__device__ __forceinline__ int last_seq(int n_seq, Le le) {
   int lo = 0, hi = n_seq;
   while (hi - lo > 1) {
-    const int mid = (lo + hi) >> 1;
-    if (q_start[mid] <= t) lo = mid;
-    else hi = mid;
+    const int step = (hi - lo + 63) / 64;
+    const int n = lo + lane_id() * step;
+    const uint64_t b = __builtin_amdgcn_ballot_w64(n < hi && le(n));
+    lo += b ? (63 - __builtin_clzll(b)) * step : 0;
+    hi = lo + step < hi ? lo + step : hi;
   }
   return lo;
 }
@@ -91,7 +95,7 @@ static __global__ __launch_bounds__(256) void k_attn_plain(AttnArgs a) {
     end = (uint32_t)n < (uint32_t)a.n_seq ? a.n_list : 0;
     if (end == 0) n = 0;
   } else {
-    n = seq_of_row(a.q_start, a.n_seq, t);
+    n = last_seq(a.n_seq, [&](int i) { return a.q_start[i] <= t; });
     if (t < a.q_start[n] || t >= a.q_start[n + 1]) return;       // nobody's row
     const int len = clamp_len(a, n);
     const int pos = a.q_pos ? a.q_pos[t] : a.seq_len[n] - a.q_start[n + 1] + t;
@@ -240,10 +244,10 @@ typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 
 // A tile of rows in LDS, bf16, D elements per row, in 16-byte chunks that are permuted inside each row so that the reads
 // below meet no bank twice: keys are read 16 bytes per row by 32 consecutive rows, values 32 bytes of 4 consecutive rows
-// per 16 lanes (the transposing read).
+// per 16 lanes (the transposing read).  The permutations are exclusive ors, so a lane's address is one number of its own
+// xor a constant of the step plus a constant: `read_key` and `read_value` are these numbers.
 template <int D>
 struct RowTile {
-  static constexpr int kChunks = D / 8;           // of a row
   static constexpr int kRowBytes = D * 2;
   __device__ static __forceinline__ int key_byte(int r, int c) {
     return r * kRowBytes + ((c ^ (D == 128 ? r & 15 : (r >> 1) & 7)) << 4);
@@ -251,22 +255,34 @@ struct RowTile {
   __device__ static __forceinline__ int value_byte(int r, int c) {
     return r * kRowBytes + ((c ^ (D == 128 ? (r & 7) << 1 : ((r >> 1) & 3) << 1)) << 4);
   }
-  // A operand of the scores: key rows r0 .. r0 + 31, contraction step kk.
-  __device__ static __forceinline__ bf16x8 key_operand(const unsigned char* tile, int r0, int kk) {
-    const int lane = lane_id(), r = r0 + (lane & 31);
-    return as_bf16x8(*reinterpret_cast<const uint4*>(tile + key_byte(r, 2 * kk + (lane >> 5))));
+  __device__ static __forceinline__ int read_key() {
+    const int lane = lane_id();
+    return key_byte(lane & 31, lane >> 5);
   }
-  // A operand of the output: columns 32 dt .. + 31, keys r0 .. r0 + 15 in the order of the weights' operand.
-  __device__ static __forceinline__ bf16x8 value_operand(const unsigned char* tile, int r0, int dt) {
+  __device__ static __forceinline__ int read_value() {
     const int lane = lane_id(), i = lane & 15;
-    const int r = r0 + 4 * (lane >> 5) + (i >> 2), c = dt * 4 + ((lane >> 4) & 1) * 2 + ((i >> 1) & 1);
-    const unsigned char* p = tile + value_byte(r, c) + (i & 1) * 8;
+    return value_byte(4 * (lane >> 5) + (i >> 2), ((lane >> 4) & 1) * 2 + ((i >> 1) & 1)) + (i & 1) * 8;
+  }
+  // A operand of the scores: key rows r0 .. r0 + 31 (r0 % 32 == 0), contraction step kk.
+  __device__ static __forceinline__ bf16x8 key_operand(const unsigned char* tile, int read_key, int r0, int kk) {
+    return as_bf16x8(*reinterpret_cast<const uint4*>(tile + (read_key ^ (kk << 5)) + r0 * kRowBytes));
+  }
+  // A operand of the output: columns 32 dt .. + 31, keys r0 .. r0 + 15 (r0 % 16 == 0) in the order of the weights' operand.
+  __device__ static __forceinline__ bf16x8 value_operand(const unsigned char* tile, int read_value, int r0, int dt) {
+    const unsigned char* p = tile + (read_value ^ (dt << 6)) + r0 * kRowBytes;
     const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)p);
     const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p + 8 * kRowBytes));
     const s16x8 v = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
     return __builtin_bit_cast(bf16x8, v);
   }
 };
+
+// Keeps what is computed from x inside the loop where it is used: a lane's addresses of a tile's steps are cheaper
+// computed again (one xor) than kept in a register each.
+__device__ __forceinline__ int renewed(int x) {
+  asm volatile("" : "+v"(x));
+  return x;
+}
 
 // 16 stored bytes of a row as they go into a tile: bf16 as they are, fp8 widened (exactly) into two chunks.
 template <int KDT>
@@ -288,7 +304,7 @@ __device__ __forceinline__ void store_chunk(unsigned char* tile, int r, int c, u
 
 __device__ __forceinline__ float max_halves(float x) {   // with lane ^ 32
   const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-  return fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1]));
+  return __builtin_elementwise_maximum(__uint_as_float(sw[0]), __uint_as_float(sw[1]));
 }
 __device__ __forceinline__ float add_halves(float x) {
   const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
@@ -322,7 +338,15 @@ struct RowState {
 // bf16 weights (whose precision is relative) hold, and most tiles need no pass over the accumulators.
 constexpr float kSlack = 8.f;
 
-// Hides the scores of a block of 32 keys that begins at `base`: key r counts where bit r of `keys` is set and the row
+// Hides the scores of the keys of a block of 32 whose bits are clear.
+__device__ __forceinline__ void hide_keys(f32x16& s, uint32_t keys) {
+  const uint32_t mine = keys >> (4 * (lane_id() >> 5));
+#pragma unroll
+  for (int i = 0; i < 16; ++i)
+    if (!(mine >> (8 * (i >> 2) + (i & 3)) & 1u)) s[i] = neg_inf();
+}
+
+// The same for a block that begins at `base`, where rows see different keys: key r counts where bit r of `keys` is set and the row
 // sees it.
 template <int D>
 __device__ __forceinline__ void hide(const RowState<D>& st, f32x16& s, uint32_t keys, int base) {
@@ -356,12 +380,21 @@ template <int D, int KDT, int NB>
 __device__ __forceinline__ void softmax_tile(RowState<D>& st, const f32x16 (&s)[NB], bf16x8 (&p)[2 * NB], float c,
                                              const float* vs) {
   const int half = lane_id() >> 5;
-  float top = neg_inf();
+  // (the IEEE 754-2019 maximum: three operands an instruction, none of them quieted first as fmaxf's are; a NaN comes
+  // through it, leaves m as it is and makes the row's sum NaN below)
+  float top4[4];
 #pragma unroll
-  for (int b = 0; b < NB; ++b)
+  for (int x = 0; x < 4; ++x) {
+    top4[x] = __builtin_elementwise_maximum(s[0][4 * x], s[0][4 * x + 1]);
+    top4[x] = __builtin_elementwise_maximum(__builtin_elementwise_maximum(top4[x], s[0][4 * x + 2]), s[0][4 * x + 3]);
 #pragma unroll
-    for (int i = 0; i < 16; i += 2) top = fmaxf(top, fmaxf(s[b][i], s[b][i + 1]));
-  top = max_halves(top) * c;
+    for (int b = 1; b < NB; ++b) {
+      top4[x] = __builtin_elementwise_maximum(__builtin_elementwise_maximum(top4[x], s[b][4 * x]), s[b][4 * x + 1]);
+      top4[x] = __builtin_elementwise_maximum(__builtin_elementwise_maximum(top4[x], s[b][4 * x + 2]), s[b][4 * x + 3]);
+    }
+  }
+  float top = __builtin_elementwise_maximum(__builtin_elementwise_maximum(top4[0], top4[1]), top4[2]);
+  top = max_halves(__builtin_elementwise_maximum(top, top4[3])) * c;
   if (__builtin_amdgcn_ballot_w64(top > st.m + kSlack)) {
     const float mn = fmaxf(st.m, top);
     const float f = __builtin_amdgcn_exp2f(st.m - (mn == neg_inf() ? 0.f : mn));
@@ -398,101 +431,70 @@ __device__ __forceinline__ void softmax_tile(RowState<D>& st, const f32x16 (&s)[
 
 // O^T += V^T P^T over NB blocks of 32 keys.
 template <int D, int NB, int NQ>
-__device__ __forceinline__ void add_values(RowState<D> (&st)[NQ], const unsigned char* tile,
+__device__ __forceinline__ void add_values(RowState<D> (&st)[NQ], const unsigned char* tile, int read_value,
                                            const bf16x8 (&p)[NQ][2 * NB]) {
 #pragma unroll
   for (int dt = 0; dt < D / 32; ++dt)
 #pragma unroll
     for (int kk = 0; kk < 2 * NB; ++kk) {
-      const bf16x8 v = RowTile<D>::value_operand(tile, 16 * kk, dt);
+      const bf16x8 v = RowTile<D>::value_operand(tile, read_value, 16 * kk, dt);
 #pragma unroll
       for (int n = 0; n < NQ; ++n) st[n].o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, p[n][kk], st[n].o[dt], 0, 0, 0);
     }
 }
 
 // A value (or, fp8, its row's scale) that is infinite or NaN must not reach the rows that do not see it, and 0 * inf
-// would.  Where some rows of a wave see less of a tile than others, the bits of its values are looked at as they are
-// stored; a tile that holds such a value (rare enough) goes through add_values_apart.
-template <int KDT>
-__device__ __forceinline__ uint32_t not_finite(uint4 x) {
-  const uint32_t w[4] = {x.x, x.y, x.z, x.w};
-  uint32_t odd = 0;
-#pragma unroll
-  for (int i = 0; i < 4; ++i)
-    odd |= KDT == 2 ? ((w[i] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u : ((w[i] & 0x7fff7fffu) + 0x00800080u) & 0x80008000u;
-  return odd;
-}
-
-// The product with zeros in the places of such values (what it gives a row that sees none of them does not depend on
-// them, to the last bit), then, one key at a time, the products of its infinities and NaN alone, added to the rows that
-// see the key.
-__device__ __forceinline__ uint32_t odd_halves(uint32_t w) {   // 0xffff over each bf16 that is inf or NaN
+// would.  Where some rows of a workgroup see less of a tile than others, such values go into the tile as zeros, and
+// afterwards to the rows that see them (add_odd_values): rare enough to read the rows again.
+__device__ __forceinline__ uint32_t odd_bf16(uint32_t w) {   // 0xffff over each bf16 that is inf or NaN
   return ((((w & 0x7fff7fffu) + 0x00800080u) & 0x80008000u) >> 15) * 0xffffu;
 }
-template <int D, int NB, int NQ>
-__device__ __forceinline__ void add_values_apart(RowState<D> (&st)[NQ], const unsigned char* tile,
-                                                 bf16x8 (&p)[NQ][2 * NB], int base) {
+__device__ __forceinline__ uint32_t odd_fp8(uint32_t w) {    // 0xff over each code that is NaN
+  return ((((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) >> 7) * 0xffu;
+}
+template <int KDT>
+__device__ __forceinline__ bool drop_odd(uint4& x) {
+  const uint4 odd = KDT == 2 ? make_uint4(odd_fp8(x.x), odd_fp8(x.y), odd_fp8(x.z), odd_fp8(x.w))
+                             : make_uint4(odd_bf16(x.x), odd_bf16(x.y), odd_bf16(x.z), odd_bf16(x.w));
+  x = make_uint4(x.x & ~odd.x, x.y & ~odd.y, x.z & ~odd.z, x.w & ~odd.w);
+  return (odd.x | odd.y | odd.z | odd.w) != 0;
+}
+
+// The infinities and NaN among the values of `n_keys` positions from `base` on, added to the rows that see them (whatever
+// their weight: it is not 0 in exact arithmetic).
+template <int D, int KDT>
+__device__ __forceinline__ void add_odd_values(const AttnArgs& a, RowState<D>& st, const int32_t* __restrict__ table, int hk,
+                                               int base, int n_keys) {
   const int half = lane_id() >> 5;
-#pragma unroll
-  for (int n = 0; n < NQ; ++n)
-#pragma unroll
-    for (int kk = 0; kk < 2 * NB; ++kk)
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const int s = base + 16 * kk + 8 * (e >> 2) + 4 * half + (e & 3);
-        if (s < st[n].lo || s > st[n].pos) p[n][kk][e] = (__bf16)0.f;
-      }
-#pragma unroll
-  for (int dt = 0; dt < D / 32; ++dt)
-#pragma unroll
-    for (int kk = 0; kk < 2 * NB; ++kk) {
-      Pack128 v;
-      v.v = RowTile<D>::value_operand(tile, 16 * kk, dt);
-      v.u = make_uint4(v.u.x & ~odd_halves(v.u.x), v.u.y & ~odd_halves(v.u.y), v.u.z & ~odd_halves(v.u.z),
-                       v.u.w & ~odd_halves(v.u.w));
-#pragma unroll
-      for (int n = 0; n < NQ; ++n)
-        st[n].o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v.v, p[n][kk], st[n].o[dt], 0, 0, 0);
-      __builtin_amdgcn_sched_barrier(0);
-    }
 #pragma unroll 1
-  for (int key = 0; key < 32 * NB; ++key) {
-    const int in = key & 15, kk = key >> 4;
-    // slot of the key: lane half (in / 4) % 2, element (in / 8) * 4 + in % 4
-    const bool mine = half == ((in >> 2) & 1);
-    const int slot = (in >> 3) * 4 + (in & 3);
-    uint32_t keep[4];
+  for (int s = base; s < base + n_keys; ++s) {
+    const bool sees = s >= st.lo && s <= st.pos;
+    if (!__builtin_amdgcn_ballot_w64(sees)) continue;         // (also: every position looked up is one of the sequence)
+    const int page = table[s >> a.page_shift], o = s & ((1 << a.page_shift) - 1);
+    if ((uint32_t)page >= (uint32_t)a.n_pages) continue;
+    const long at = page * a.page_stride + o * a.token_stride + hk * a.head_stride;
+    const float scale = KDT == 2 ? a.v_scale[(((long)page << a.page_shift) + o) * a.H_kv + hk] : 1.f;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) keep[e] = mine && slot >> 1 == e ? 0xffffu << (16 * (slot & 1)) : 0u;
+    for (int dt = 0; dt < D / 32; ++dt)
 #pragma unroll
-    for (int n = 0; n < NQ; ++n) {
-      Pack128 w;
-      w.v = p[n][0];
+      for (int j = 0; j < 4; ++j) {
+        const int e = dt * 32 + 8 * j + 4 * half;
+        uint2 w;
+        if constexpr (KDT == 2) w = fp8x4_to_bf16x4(*reinterpret_cast<const uint32_t*>((const uint8_t*)a.v + at + e));
+        else w = *reinterpret_cast<const uint2*>((const uint16_t*)a.v + at + e);
+        const float v[4] = {__uint_as_float(w.x << 16), __uint_as_float(w.x & 0xffff0000u), __uint_as_float(w.y << 16),
+                            __uint_as_float(w.y & 0xffff0000u)};
 #pragma unroll
-      for (int x = 1; x < 2 * NB; ++x)
-        if (kk == x) w.v = p[n][x];
-      w.u = make_uint4(w.u.x & keep[0], w.u.y & keep[1], w.u.z & keep[2], w.u.w & keep[3]);
-      const bool sees = base + key >= st[n].lo && base + key <= st[n].pos;
-#pragma unroll
-      for (int dt = 0; dt < D / 32; ++dt) {
-        Pack128 v;
-        v.v = RowTile<D>::value_operand(tile, 16 * kk, dt);
-        v.u = make_uint4(v.u.x & odd_halves(v.u.x) & keep[0], v.u.y & odd_halves(v.u.y) & keep[1],
-                         v.u.z & odd_halves(v.u.z) & keep[2], v.u.w & odd_halves(v.u.w) & keep[3]);
-        f32x16 one;
-#pragma unroll
-        for (int i = 0; i < 16; ++i) one[i] = 0.f;
-        one = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v.v, w.v, one, 0, 0, 0);
-#pragma unroll
-        for (int i = 0; i < 16; ++i) st[n].o[dt][i] += sees ? one[i] : 0.f;
-        __builtin_amdgcn_sched_barrier(0);
+        for (int x = 0; x < 4; ++x) {
+          const float y = KDT == 2 ? v[x] * scale : v[x];
+          if (sees && !(__builtin_fabsf(y) < __builtin_inff())) st.o[dt][4 * j + x] += y;
+        }
       }
-    }
   }
 }
 
 template <int D, int NB, int NQ>
-__device__ __forceinline__ void score_tile(const RowState<D> (&st)[NQ], const unsigned char* tile, f32x16 (&s)[NQ][NB]) {
+__device__ __forceinline__ void score_tile(const RowState<D> (&st)[NQ], const unsigned char* tile, int read_key, f32x16 (&s)[NQ][NB]) {
 #pragma unroll
   for (int b = 0; b < NB; ++b) {
 #pragma unroll
@@ -501,7 +503,7 @@ __device__ __forceinline__ void score_tile(const RowState<D> (&st)[NQ], const un
       for (int i = 0; i < 16; ++i) s[n][b][i] = 0.f;
 #pragma unroll
     for (int kk = 0; kk < D / 16; ++kk) {
-      const bf16x8 a = RowTile<D>::key_operand(tile, 32 * b, kk);
+      const bf16x8 a = RowTile<D>::key_operand(tile, read_key, 32 * b, kk);
 #pragma unroll
       for (int n = 0; n < NQ; ++n) s[n][b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, st[n].q[kk], s[n][b], 0, 0, 0);
     }
@@ -536,23 +538,24 @@ struct RowUnit {
 };
 template <int ROWS>
 __device__ __forceinline__ RowUnit find_unit(const AttnArgs& a, int unit) {
-  int lo = 0, hi = a.n_seq;
-  const int lane = lane_id();
-  while (hi - lo > 1) {              // 64 candidates at a time
-    const int step = (hi - lo + 63) / 64;
-    const int n = lo + lane * step;
-    const bool le = n < hi && (long)a.q_start[n] * a.G / ROWS + n <= unit;
-    const uint64_t b = __builtin_amdgcn_ballot_w64(le);
-    const int last = b ? 63 - __builtin_clzll(b) : 0;
-    lo += last * step;
-    hi = lo + step < hi ? lo + step : hi;
-  }
+  const int lo = last_seq(a.n_seq, [&](int i) { return (long)a.q_start[i] * a.G / ROWS + i <= unit; });
   RowUnit u;
   u.n = lo;
   u.t_begin = a.q_start[lo];
   u.t_end = a.q_start[lo + 1];
   u.r0 = (unit - ((long)u.t_begin * a.G / ROWS + lo)) * ROWS;
   return u;
+}
+
+// Part `split` of the tiles begin .. end: consecutive runs of equal length, `least` tiles at least, so that the last parts
+// of a short sequence are empty.
+__device__ __forceinline__ void take_part(int& begin, int& end, int split, int splits, int least) {
+  const uint32_t n = (uint32_t)(end - begin), share = (n + (uint32_t)splits - 1) / (uint32_t)splits;
+  const uint32_t per = share < (uint32_t)least ? (uint32_t)least : share;
+  const uint64_t first = (uint64_t)per * (uint32_t)split;
+  const int e = end;
+  begin = first < n ? begin + (int)first : e;
+  end = e - begin > (int)per ? begin + (int)per : e;
 }
 
 // One result row: 4 columns at e of (t, h) row r, sums with maximum m and weight sum l.
@@ -573,11 +576,12 @@ __device__ __forceinline__ void store_result(const AttnArgs& a, int split, long 
   }
 }
 
-// ---- few rows per sequence, or lists: keys split over the waves --------------------------------
-// A workgroup of 4 waves takes NQ * 32 query rows of one KV head and a part of their keys.  Every wave works alone on its
-// own tiles of 32 keys (every fourth): the next tile's rows are on their way into registers while the present one, in the
-// wave's own 32 * D * 4 bytes of LDS, is multiplied; the waves' results are joined at the end.  Bound by memory: 4 D bytes
-// (bf16) per key and KV head, whatever the number of rows.
+// ---- one token at a time, over a range or a list: keys split over the waves -----------------------
+// A workgroup of 4 waves takes one token, up to NQ * 32 heads of one KV head's group and a part of the keys.  Every wave
+// works alone on its own tiles of 32 keys (every fourth): the next tile's rows are on their way into registers while the
+// present one, in the wave's own 32 * D * 4 bytes of LDS, is multiplied; the waves' results are joined at the end.  All
+// rows see the same keys, so a row outside is a row of zeros and a score of -inf for everybody.  Bound by memory: 4 D
+// bytes (bf16) per key and KV head, whatever the number of heads.
 constexpr int kRowWaves = 4;
 
 template <int D, int KDT>
@@ -600,116 +604,97 @@ static __global__ __launch_bounds__(256, NQ == 1 ? 2 : 1) void k_attn_rows(AttnA
   float* sc = reinterpret_cast<float*>(vt + Geo::kTile);                       // 32 key scales, 32 value scales
   float* join = reinterpret_cast<float*>(lds + kRowWaves * Geo::kWaveLds);     // [wave][32][2]
 
-  long id = blockIdx.x;
-  const int hk = (int)(id % a.H_kv);
-  id /= a.H_kv;
-  const int split = (int)(id % a.splits);
-  const int unit = (int)(id / a.splits);
-  int n, t_begin, t_end, len;
-  long r0, rows;                          // the tile's first row and the number of rows there are
+  uint32_t id = blockIdx.x;
+  const int hk = (int)(id % (uint32_t)a.H_kv);
+  id /= (uint32_t)a.H_kv;
+  const int split = (int)(id % (uint32_t)a.splits);
+  const int unit = (int)(id / (uint32_t)a.splits);
+  const int head_tiles = (a.G + 32 * NQ - 1) / (32 * NQ);
+  const int t = unit / head_tiles, r0 = (unit - t * head_tiles) * 32 * NQ;
+  int n, len, lo = 0, pos = 0;
   if constexpr (LIST) {
-    const int tiles = (a.G + 32 * NQ - 1) / (32 * NQ);
-    t_begin = unit / tiles;
-    t_end = t_begin + 1;
-    r0 = (unit - (long)t_begin * tiles) * 32 * NQ;
-    rows = a.G;
-    n = a.q_seq ? a.q_seq[t_begin] : 0;
+    n = a.q_seq ? a.q_seq[t] : 0;
     const bool none = (uint32_t)n >= (uint32_t)a.n_seq;
     n = none ? 0 : n;
     len = none ? 0 : clamp_len(a, n);
   } else {
-    const RowUnit u = find_unit<32 * NQ>(a, unit);
-    n = u.n;
-    t_begin = u.t_begin;
-    t_end = u.t_end;
-    r0 = u.r0;
-    rows = (long)(t_end - t_begin) * a.G;
-    if (r0 < 0 || r0 >= rows || t_begin < 0 || t_end > a.T) return;
+    n = last_seq(a.n_seq, [&](int i) { return a.q_start[i] <= t; });
+    const int t_end = a.q_start[n + 1];
+    if (t < a.q_start[n] || t >= t_end) return;
     len = clamp_len(a, n);
+    const Seen s = seen_by(a, n, len, t, t_end);
+    lo = s.lo;
+    pos = s.pos;
   }
   const int32_t* __restrict__ table = a.table + (long)n * a.max_pages;
-
-  // the rows of this lane's columns (rows beyond the last one repeat it and are not stored)
   RowState<D> st[NQ];
-  int pos_min = 0x7fffffff, pos_max = -1, lo_min = 0x7fffffff, lo_max = 0;
 #pragma unroll
-  for (int q = 0; q < NQ; ++q) {
-    long r = r0 + q * 32 + col;
-    if (r >= rows) r = rows - 1;
-    const int t = t_begin + (int)(r / a.G), h = hk * a.G + (int)(r % a.G);
+  for (int q = 0; q < NQ; ++q) {          // (columns beyond the last head repeat it and are not stored)
+    int r = r0 + q * 32 + col;
+    if (r >= a.G) r = a.G - 1;
     st[q].clear();
-    st[q].load_q((const uint16_t*)a.q + ((long)t * a.H + h) * D);
-    if constexpr (LIST) {
-      st[q].pos = 0x7fffffff;
-      st[q].lo = 0;
-    } else {
-      const Seen s = seen_by(a, n, len, t, t_end);
-      st[q].pos = s.pos;
-      st[q].lo = s.lo;
-      pos_min = s.pos < pos_min ? s.pos : pos_min;
-      pos_max = s.pos > pos_max ? s.pos : pos_max;
-      lo_min = s.lo < lo_min ? s.lo : lo_min;
-      lo_max = s.lo > lo_max ? s.lo : lo_max;
-    }
+    st[q].load_q((const uint16_t*)a.q + ((long)t * a.H + hk * a.G + r) * D);
   }
   int begin, end;                         // tiles of 32 keys (list entries); range tiles begin at multiples of 32
-  bool differ = false;                    // whether some rows see what others do not
   if constexpr (LIST) {
     begin = 0;
     end = len > 0 ? (a.n_list + 31) / 32 : 0;
   } else {
-    pos_min = wave_min_int(pos_min);
-    pos_max = wave_max_int(pos_max);
-    lo_min = wave_min_int(lo_min);
-    lo_max = wave_max_int(lo_max);
-    differ = pos_min != pos_max || lo_min != lo_max;
-    begin = lo_min >> 5;
-    end = (pos_max + 32) >> 5;
-    if (end < begin) end = begin;
+    begin = lo >> 5;
+    end = (pos + 32) >> 5;
+    if (pos < 0 || end < begin) end = begin;
   }
   if (a.splits > 1) {
-    // parts of at least 8 tiles (two per wave); the last parts of a short sequence are empty
-    const long nt = end - begin;
-    const long parts = nt < 8L * a.splits ? (nt + 7) / 8 : a.splits;
-    const int b0 = begin;
-    if (split < parts) {
-      begin = b0 + (int)(nt * split / parts);
-      end = b0 + (int)(nt * (split + 1) / parts);
-    } else {
-      end = begin;
-    }
+    take_part(begin, end, split, a.splits, 8);      // of at least two tiles per wave
   }
 
   // page lookups run two tiles ahead of the rows, list entries three
   auto position = [&](int tile) {         // of key `col` of a tile, or -1
     if (tile >= end) return -1;
     const int c = tile * 32 + col;
-    if constexpr (LIST) return c < a.n_list ? a.list[(long)t_begin * a.n_list + c] : -1;
+    if constexpr (LIST) return c < a.n_list ? a.list[(long)t * a.n_list + c] : -1;
     else return c;
   };
   auto page_of = [&](int s) {
-    const bool ok = LIST ? s >= 0 && s < len : s >= lo_min && s <= pos_max;
+    const bool ok = LIST ? s >= 0 && s < len : s >= lo && s <= pos;
     return ok ? table[s >> a.page_shift] : -1;
   };
-  const unsigned char* __restrict__ kbase = (const unsigned char*)a.k + hk * a.head_stride * (KDT == 2 ? 1 : 2);
-  const unsigned char* __restrict__ vbase = (const unsigned char*)a.v + hk * a.head_stride * (KDT == 2 ? 1 : 2);
+  constexpr int kBytes = KDT == 2 ? 1 : 2;
+  const unsigned char* __restrict__ kbase = (const unsigned char*)a.k + hk * a.head_stride * kBytes;
+  const unsigned char* __restrict__ vbase = (const unsigned char*)a.v + hk * a.head_stride * kBytes;
   uint4 kr[Geo::kNi], vr[Geo::kNi];
   float scale = 0.f;
   uint32_t valid = 0;                     // rows of the tile in registers that there are
+  // a tile inside one page that every row of it reaches into is one address and a lane's part of it
+  const bool one_page = !LIST && a.page_shift >= 5;
+  const int first_inside = (lo + 31) & ~31, last_inside = pos - 31;
+  const long lane_at = (lane / Geo::kCpr) * a.token_stride * kBytes + lane % Geo::kCpr * 16;
   auto request = [&](int s, int page) {
+    const int s0 = __builtin_amdgcn_readfirstlane(s), page0 = __builtin_amdgcn_readfirstlane(page);
+    const int o = s & ((1 << a.page_shift) - 1);
     const bool ok = (uint32_t)page < (uint32_t)a.n_pages;
     valid = (uint32_t)__builtin_amdgcn_ballot_w64(ok);
-    const int o = s & ((1 << a.page_shift) - 1);
-    const long row = ok ? (page * a.page_stride + o * a.token_stride) * (KDT == 2 ? 1 : 2) : -1;
+    if (one_page && s0 >= first_inside && s0 <= last_inside && (uint32_t)page0 < (uint32_t)a.n_pages) {
+      const long at = (page0 * a.page_stride + (s0 & ((1 << a.page_shift) - 1)) * a.token_stride) * kBytes;
+      const unsigned char *ks = kbase + at, *vs = vbase + at;
+      const long step = Geo::kRpi * a.token_stride * kBytes;
 #pragma unroll
-    for (int i = 0; i < Geo::kNi; ++i) {
-      const int r = i * Geo::kRpi + lane / Geo::kCpr;
-      const uint32_t lo = __shfl((uint32_t)row, r), hi = __shfl((uint32_t)((uint64_t)row >> 32), r);
-      const long at = (long)((uint64_t)hi << 32 | lo);
-      kr[i] = vr[i] = make_uint4(0, 0, 0, 0);
-      if (at >= 0) {
-        kr[i] = *reinterpret_cast<const uint4*>(kbase + at + lane % Geo::kCpr * 16);
-        vr[i] = *reinterpret_cast<const uint4*>(vbase + at + lane % Geo::kCpr * 16);
+      for (int i = 0; i < Geo::kNi; ++i) {
+        kr[i] = *reinterpret_cast<const uint4*>(ks + i * step + lane_at);
+        vr[i] = *reinterpret_cast<const uint4*>(vs + i * step + lane_at);
+      }
+    } else {
+      const long row = ok ? (page * a.page_stride + o * a.token_stride) * kBytes : -1;
+#pragma unroll
+      for (int i = 0; i < Geo::kNi; ++i) {
+        const int r = i * Geo::kRpi + lane / Geo::kCpr;
+        const uint32_t lo = __shfl((uint32_t)row, r), hi = __shfl((uint32_t)((uint64_t)row >> 32), r);
+        const long at = (long)((uint64_t)hi << 32 | lo);
+        kr[i] = vr[i] = make_uint4(0, 0, 0, 0);
+        if (at >= 0) {
+          kr[i] = *reinterpret_cast<const uint4*>(kbase + at + lane % Geo::kCpr * 16);
+          vr[i] = *reinterpret_cast<const uint4*>(vbase + at + lane % Geo::kCpr * 16);
+        }
       }
     }
     if constexpr (KDT == 2) {
@@ -718,6 +703,7 @@ static __global__ __launch_bounds__(256, NQ == 1 ? 2 : 1) void k_attn_rows(AttnA
     }
   };
 
+  const int read_key = RowTile<D>::read_key(), read_value = RowTile<D>::read_value();
   int tile = begin + wave;
   int s1 = position(tile), s2 = position(tile + kRowWaves);
   request(s1, page_of(s1));
@@ -725,13 +711,6 @@ static __global__ __launch_bounds__(256, NQ == 1 ? 2 : 1) void k_attn_rows(AttnA
   int s3 = position(tile + 2 * kRowWaves);
   for (; tile < end; tile += kRowWaves) {
     const uint32_t keys = valid;
-    bool apart = false;
-    if (!LIST && differ) {                // rows that nobody sees are zeros by now
-      uint32_t odd = KDT == 2 && half && __builtin_isfpclass(scale, 0x207) ? 1u : 0u;
-#pragma unroll
-      for (int i = 0; i < Geo::kNi; ++i) odd |= not_finite<KDT>(vr[i]);
-      apart = __builtin_amdgcn_ballot_w64(odd != 0) != 0;
-    }
 #pragma unroll
     for (int i = 0; i < Geo::kNi; ++i) {
       const int r = i * Geo::kRpi + lane / Geo::kCpr;
@@ -747,20 +726,19 @@ static __global__ __launch_bounds__(256, NQ == 1 ? 2 : 1) void k_attn_rows(AttnA
 
     f32x16 s[NQ][1];
     bf16x8 p[NQ][2];
-    score_tile<D, 1, NQ>(st, kt, s);
+    score_tile<D, 1, NQ>(st, kt, renewed(read_key), s);
     if constexpr (KDT == 2) {
 #pragma unroll
       for (int q = 0; q < NQ; ++q) scale_scores<1>(s[q], sc);
     }
-    const int base = LIST ? 0 : tile * 32;
-    if (keys != 0xffffffffu || (!LIST && (base + 31 > pos_min || base < lo_max))) {
+    if (keys != 0xffffffffu) {
+      asm volatile("");                    // (a branch, not selects for every tile)
 #pragma unroll
-      for (int q = 0; q < NQ; ++q) hide(st[q], s[q][0], keys, base);
+      for (int q = 0; q < NQ; ++q) hide_keys(s[q][0], keys);
     }
 #pragma unroll
     for (int q = 0; q < NQ; ++q) softmax_tile<D, KDT, 1>(st[q], s[q], p[q], a.scale_log2, sc + 32);
-    if (!LIST && apart) add_values_apart<D, 1, NQ>(st, vt, p, base);
-    else add_values<D, 1, NQ>(st, vt, p);
+    add_values<D, 1, NQ>(st, vt, renewed(read_value), p);
     wave_lds_order();
   }
 
@@ -790,9 +768,9 @@ static __global__ __launch_bounds__(256, NQ == 1 ? 2 : 1) void k_attn_rows(AttnA
       for (int i = 0; i < 16; ++i)
         part[(wave * D + dt * 32 + 8 * (i >> 2) + 4 * half + (i & 3)) * 32 + col] = st[q].o[dt][i] * f;
     __syncthreads();
-    const long r = r0 + q * 32 + col;
-    if (r < rows) {
-      const long row = (long)(t_begin + (int)(r / a.G)) * a.H + hk * a.G + (int)(r % a.G);
+    const int r = r0 + q * 32 + col;
+    if (r < a.G) {
+      const long row = (long)t * a.H + hk * a.G + r;
 #pragma unroll
       for (int j = 0; j < D / 32; ++j) {
         const int e = ((threadIdx.x >> 5) * (D / 32) + j) * 4;
@@ -833,11 +811,11 @@ static __global__ __launch_bounds__(512, 2) void k_attn_chunk(AttnArgs a) {
   extern __shared__ __align__(16) unsigned char lds[];
   const int lane = lane_id(), wave = threadIdx.x >> 6, half = lane >> 5, col = lane & 31;
 
-  long id = blockIdx.x;
-  const int hk = (int)(id % a.H_kv);
-  id /= a.H_kv;
-  const int split = (int)(id % a.splits);
-  const RowUnit u = find_unit<kChunkRows>(a, (int)(id / a.splits));
+  uint32_t id = blockIdx.x;
+  const int hk = (int)(id % (uint32_t)a.H_kv);
+  id /= (uint32_t)a.H_kv;
+  const int split = (int)(id % (uint32_t)a.splits);
+  const RowUnit u = find_unit<kChunkRows>(a, (int)(id / (uint32_t)a.splits));
   const int n = u.n, t_begin = u.t_begin, t_end = u.t_end;
   const long r0 = u.r0, rows = (long)(t_end - t_begin) * a.G;
   if (r0 < 0 || r0 >= rows || t_begin < 0 || t_end > a.T) return;
@@ -879,15 +857,7 @@ static __global__ __launch_bounds__(512, 2) void k_attn_chunk(AttnArgs a) {
   int begin = wg_lo / kChunkKeys, end = (wg_pos + kChunkKeys) / kChunkKeys;
   if (wg_pos < 0 || end < begin) end = begin;
   if (a.splits > 1) {
-    const long nt = end - begin;
-    const long parts = nt < 4L * a.splits ? (nt + 3) / 4 : a.splits;     // of at least 4 tiles
-    const int b0 = begin;
-    if (split < parts) {
-      begin = b0 + (int)(nt * split / parts);
-      end = b0 + (int)(nt * (split + 1) / parts);
-    } else {
-      end = begin;
-    }
+    take_part(begin, end, split, a.splits, 4);
   }
 
   // this thread's chunks of a tile: chunk x = i * 512 + thread, keys first, then values
@@ -932,12 +902,23 @@ static __global__ __launch_bounds__(512, 2) void k_attn_chunk(AttnArgs a) {
     }
   };
   uint64_t* masks = reinterpret_cast<uint64_t*>(lds + 2 * Geo::kBuffer);     // of the two buffers
-  int* odd = reinterpret_cast<int*>(masks + 2);                               // tile with infinities or NaN that not
-  if (threadIdx.x < 2) odd[threadIdx.x] = -1;                                 // every row of the workgroup sees
+  int* odd = reinterpret_cast<int*>(masks + 2);                               // tile with infinities or NaN dropped
+  if (threadIdx.x < 2) odd[threadIdx.x] = -1;
   __syncthreads();
   auto deposit = [&](int buffer, int tile) {
     unsigned char* kt = lds + buffer * Geo::kBuffer;
     unsigned char* vt = kt + Geo::kTile;
+    if (tile * kChunkKeys + kChunkKeys - 1 > wg_pos_min || tile * kChunkKeys < wg_lo_max) {
+      bool found = false;
+      if (KDT == 2 && threadIdx.x >= kChunkKeys && !(__builtin_fabsf(scale) < __builtin_inff())) {
+        scale = 0.f;
+        found = true;
+      }
+#pragma unroll
+      for (int i = 0; i < Geo::kPerThread; ++i)
+        if (is_value(i)) found |= drop_odd<KDT>(x[i]);
+      if (found) odd[buffer] = tile;
+    }
 #pragma unroll
     for (int i = 0; i < Geo::kPerThread; ++i) {
       const int c = threadIdx.x % Geo::kCpr;
@@ -947,14 +928,9 @@ static __global__ __launch_bounds__(512, 2) void k_attn_chunk(AttnArgs a) {
     if constexpr (KDT == 2)
       if (threadIdx.x < 2 * kChunkKeys) reinterpret_cast<float*>(vt + Geo::kTile)[threadIdx.x] = scale;
     if (threadIdx.x == 0) masks[buffer] = there;
-    if (tile * kChunkKeys + kChunkKeys - 1 > wg_pos_min || tile * kChunkKeys < wg_lo_max) {
-      bool found = KDT == 2 && threadIdx.x >= kChunkKeys && __builtin_isfpclass(scale, 0x207);
-#pragma unroll
-      for (int i = 0; i < Geo::kPerThread; ++i) found |= is_value(i) && not_finite<KDT>(x[i]) != 0;
-      if (found) odd[buffer] = tile;
-    }
   };
 
+  const int read_key = RowTile<D>::read_key(), read_value = RowTile<D>::read_value();
   lookup(begin);
   request(begin);
   lookup(begin + 1);
@@ -973,15 +949,16 @@ static __global__ __launch_bounds__(512, 2) void k_attn_chunk(AttnArgs a) {
       const uint32_t keys[2] = {(uint32_t)mask, (uint32_t)(mask >> 32)};
       f32x16 s[1][2];
       bf16x8 p[1][4];
-      score_tile<D, 2, 1>(st, kt, s);
+      score_tile<D, 2, 1>(st, kt, renewed(read_key), s);
       if constexpr (KDT == 2) scale_scores<2>(s[0], sc);
       if ((keys[0] & keys[1]) != 0xffffffffu || base + kChunkKeys - 1 > pos_min || base < lo_max) {
+        asm volatile("");                  // (a branch, not 32 selects for every tile)
         hide(st[0], s[0][0], keys[0], base);
         hide(st[0], s[0][1], keys[1], base + 32);
       }
       softmax_tile<D, KDT, 2>(st[0], s[0], p[0], a.scale_log2, sc + kChunkKeys);
-      if (odd[buffer] == tile) add_values_apart<D, 2, 1>(st, vt, p, base);
-      else add_values<D, 2, 1>(st, vt, p);
+      add_values<D, 2, 1>(st, vt, renewed(read_value), p);
+      if (odd[buffer] == tile) add_odd_values<D, KDT>(a, st[0], table, hk, base, kChunkKeys);
     }
     if (tile + 1 < end) {
       deposit(buffer ^ 1, tile + 1);

@@ -57,7 +57,7 @@ int check_attention(const hisa_queries* q, const hisa_cache* c, int32_t k) {
 enum AttnKernel { ATTN_PLAIN, ATTN_ROWS, ATTN_CHUNK };
 struct AttnPlan {
   AttnKernel kernel;
-  int row_tiles;      // ATTN_ROWS: 32 query rows each, per wave
+  int row_tiles;      // ATTN_ROWS: 32 heads each, per wave
   long units;         // tiles of query rows, of one KV head
   int splits;         // parts of their keys
   size_t ws_bytes;
@@ -73,11 +73,10 @@ AttnPlan plan_attention(const hisa_queries* q, const hisa_cache* c, int32_t k) {
     p.units = T * ((G + kPlainHeads - 1) / kPlainHeads);
     most = (keys + 511) / 512;
     want = 1024;
-  } else if (k || T * G <= 64L * c->n_seq) {
+  } else if (k || T <= c->n_seq) {
     p.kernel = ATTN_ROWS;
-    p.row_tiles = (k ? G > 32 : T * G > 32L * c->n_seq) ? 2 : 1;
-    const long rows = 32 * p.row_tiles;
-    p.units = k ? T * ((G + rows - 1) / rows) : T * G / rows + c->n_seq;
+    p.row_tiles = G > 32 ? 2 : 1;
+    p.units = T * ((G + 32 * p.row_tiles - 1) / (32 * p.row_tiles));
     most = (keys + 255) / 256;
     want = 2048;
   } else {
