@@ -243,8 +243,8 @@ typedef short s16x8 __attribute__((ext_vector_type(8)));
 typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 
 // A tile of rows in LDS, bf16, D elements per row, in 16-byte chunks that are permuted inside each row so that the reads
-// below meet no bank twice: keys are read 16 bytes per row by 32 consecutive rows, values 32 bytes of 4 consecutive rows
-// per 16 lanes (the transposing read).  The permutations are exclusive ors, so a lane's address is one number of its own
+// below meet no bank twice: keys are read 16 bytes per row by 32 consecutive rows, values 64 bytes of 4 consecutive rows
+// per 32 lanes (the transposing read).  The permutations are exclusive ors, so a lane's address is one number of its own
 // xor a constant of the step plus a constant: `read_key` and `read_value` are these numbers.
 template <int D>
 struct RowTile {
@@ -253,7 +253,7 @@ struct RowTile {
     return r * kRowBytes + ((c ^ (D == 128 ? r & 15 : (r >> 1) & 7)) << 4);
   }
   __device__ static __forceinline__ int value_byte(int r, int c) {
-    return r * kRowBytes + ((c ^ (D == 128 ? (r & 7) << 1 : ((r >> 1) & 3) << 1)) << 4);
+    return r * kRowBytes + ((c ^ (D == 128 ? (r & 3) << 2 : ((r >> 1) & 1) << 2)) << 4);
   }
   __device__ static __forceinline__ int read_key() {
     const int lane = lane_id();
@@ -460,28 +460,26 @@ __device__ __forceinline__ bool drop_odd(uint4& x) {
   return (odd.x | odd.y | odd.z | odd.w) != 0;
 }
 
-// The infinities and NaN among the values of `n_keys` positions from `base` on, added to the rows that see them (whatever
-// their weight: it is not 0 in exact arithmetic).
+// The infinities and NaN among the values of the 64 positions from `base` on, added to the rows that see them (whatever
+// their weight: it is not 0 in exact arithmetic).  offsets (bytes behind vbase, -1: none), slots: where the rows lie.
 template <int D, int KDT>
-__device__ __forceinline__ void add_odd_values(const AttnArgs& a, RowState<D>& st, const int32_t* __restrict__ table, int hk,
-                                               int base, int n_keys) {
+__device__ __forceinline__ void add_odd_values(RowState<D>& st, const unsigned char* __restrict__ vbase, const long* offsets,
+                                               const int* slots, const float* __restrict__ v_scale, int H_kv, int base) {
   const int half = lane_id() >> 5;
 #pragma unroll 1
-  for (int s = base; s < base + n_keys; ++s) {
-    const bool sees = s >= st.lo && s <= st.pos;
-    if (!__builtin_amdgcn_ballot_w64(sees)) continue;         // (also: every position looked up is one of the sequence)
-    const int page = table[s >> a.page_shift], o = s & ((1 << a.page_shift) - 1);
-    if ((uint32_t)page >= (uint32_t)a.n_pages) continue;
-    const long at = page * a.page_stride + o * a.token_stride + hk * a.head_stride;
-    const float scale = KDT == 2 ? a.v_scale[(((long)page << a.page_shift) + o) * a.H_kv + hk] : 1.f;
+  for (int key = 0; key < 64; ++key) {
+    const bool sees = base + key >= st.lo && base + key <= st.pos && offsets[key] >= 0;
+    if (!__builtin_amdgcn_ballot_w64(sees)) continue;
+    const unsigned char* row = vbase + offsets[key];
+    const float scale = KDT == 2 ? v_scale[(long)slots[key] * H_kv] : 1.f;
 #pragma unroll
     for (int dt = 0; dt < D / 32; ++dt)
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         const int e = dt * 32 + 8 * j + 4 * half;
         uint2 w;
-        if constexpr (KDT == 2) w = fp8x4_to_bf16x4(*reinterpret_cast<const uint32_t*>((const uint8_t*)a.v + at + e));
-        else w = *reinterpret_cast<const uint2*>((const uint16_t*)a.v + at + e);
+        if constexpr (KDT == 2) w = fp8x4_to_bf16x4(*reinterpret_cast<const uint32_t*>(row + e));
+        else w = *reinterpret_cast<const uint2*>(row + 2 * e);
         const float v[4] = {__uint_as_float(w.x << 16), __uint_as_float(w.x & 0xffff0000u), __uint_as_float(w.y << 16),
                             __uint_as_float(w.y & 0xffff0000u)};
 #pragma unroll
@@ -489,6 +487,7 @@ __device__ __forceinline__ void add_odd_values(const AttnArgs& a, RowState<D>& s
           const float y = KDT == 2 ? v[x] * scale : v[x];
           if (sees && !(__builtin_fabsf(y) < __builtin_inff())) st.o[dt][4 * j + x] += y;
         }
+        __builtin_amdgcn_sched_barrier(0);
       }
   }
 }
@@ -507,6 +506,40 @@ __device__ __forceinline__ void score_tile(const RowState<D> (&st)[NQ], const un
 #pragma unroll
       for (int n = 0; n < NQ; ++n) s[n][b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, st[n].q[kk], s[n][b], 0, 0, 0);
     }
+  }
+}
+
+// Scores of one tile of 64 keys and values of the one before, as one stream of D / 4 products.  The operands of the next
+// eight are under way from LDS while one is multiplied: the order is pinned, because the compiler's own asks for four at
+// most and the matrix unit then waits for LDS after every second product.  Consecutive products have different
+// accumulators.
+template <int D>
+__device__ __forceinline__ void products(RowState<D>& st, const unsigned char* kt, int read_key, f32x16 (&s)[2],
+                                         const unsigned char* vt, int read_value, const bf16x8 (&p)[4]) {
+  constexpr int kAhead = 8, kScores = D / 8, kTiles = D / 32;
+  bf16x8 f[kAhead];
+  auto operand = [&](int i) {
+    return i < kScores ? RowTile<D>::key_operand(kt, read_key, 32 * (i & 1), i >> 1)
+                       : RowTile<D>::value_operand(vt, read_value, 16 * ((i - kScores) / kTiles), (i - kScores) % kTiles);
+  };
+#pragma unroll
+  for (int i = 0; i < kAhead; ++i) f[i] = operand(i);
+#pragma unroll
+  for (int i = 0; i < 2 * kScores; ++i) {
+    const bf16x8 x = f[i % kAhead];
+    if (i < kScores) {
+      f32x16 c = s[i & 1];
+      if (i < 2) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) c[e] = 0.f;
+      }
+      s[i & 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, st.q[i >> 1], c, 0, 0, 0);
+    } else {
+      const int j = i - kScores;
+      st.o[j % kTiles] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, p[j / kTiles], st.o[j % kTiles], 0, 0, 0);
+    }
+    if (i + kAhead < 2 * kScores) f[i % kAhead] = operand(i + kAhead);
+    __builtin_amdgcn_sched_barrier(0);
   }
 }
 
@@ -529,12 +562,21 @@ __device__ __forceinline__ int wave_min_int(int x) {
   return __builtin_amdgcn_readfirstlane((int)(wave_min((uint32_t)x ^ 0x80000000u) ^ 0x80000000u));
 }
 
+// A barrier of the workgroup that orders LDS alone: __syncthreads would also wait for every global load under way.
+__device__ __forceinline__ void lds_barrier() {
+  __builtin_amdgcn_sched_barrier(0);
+  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_sched_barrier(0);
+}
+
 // The row tile `unit` of rows_per tile rows: sequence and first row in it, or -1.  Tiles are numbered so that sequence n
 // begins at floor(q_start[n] * G / rows_per) + n: at most one number per sequence stays unused, and the grid needs T,
 // n_seq and G alone.
 struct RowUnit {
   int n, t_begin, t_end;   // sequence and its token rows
-  long r0;                 // first row (token, head) of the tile, in the sequence
+  int r0;                  // first row (token, head) of the tile, in the sequence
 };
 template <int ROWS>
 __device__ __forceinline__ RowUnit find_unit(const AttnArgs& a, int unit) {
@@ -543,7 +585,7 @@ __device__ __forceinline__ RowUnit find_unit(const AttnArgs& a, int unit) {
   u.n = lo;
   u.t_begin = a.q_start[lo];
   u.t_end = a.q_start[lo + 1];
-  u.r0 = (unit - ((long)u.t_begin * a.G / ROWS + lo)) * ROWS;
+  u.r0 = (unit - (int)((long)u.t_begin * a.G / ROWS + lo)) * ROWS;
   return u;
 }
 
@@ -791,9 +833,17 @@ static __global__ __launch_bounds__(256, NQ == 1 ? 2 : 1) void k_attn_rows(AttnA
 
 // ---- many rows per sequence ----------------------------------------------------------------------
 // A workgroup of 8 waves takes 256 query rows of one KV head (32 per wave) and a part of their keys, in tiles of 64 keys
-// that all waves multiply from LDS: two buffers, one barrier per tile, the tile after next on its way into registers.
-// Bound by the matrix units (4 D flop per visible pair): 8 waves are two per SIMD, so that one's softmax runs under the
-// other's products.
+// that all waves multiply from LDS (two buffers for keys and for values).  Bound by the matrix units (4 D flop per visible
+// pair).  Each SIMD holds two waves, one of the first four and one of the last four, half a tile apart: in every phase,
+// between two barriers, one of them runs its products (scores of tile i, values of tile i - 1) while the other turns its
+// scores into weights and moves its share of the next rows from registers to LDS.  Running together, both would wait for
+// the matrix unit first and leave it idle afterwards.
+//
+// Phase 2 i + g is the products of group g for tile i, phase 2 i + 1 + g its softmax.  Keys of tile i are read in phases
+// 2 i and 2 i + 1, values of tile i in phases 2 i + 2 and 2 i + 3.  Step i (keys of tile i + 1, values of tile i, written in
+// phases 2 i and 2 i + 1: by the last four waves in the softmax phase of tile i - 1, by the first four in that of tile i)
+// therefore finds its buffers unread.  Scales go with the keys and are read in phases 2 i + 1 and 2 i + 2 by the softmax;
+// waves 0 and 1 alone write them, in phase 2 i + 1 of step i, when those of tile i - 1, in the same buffer, are done with.
 constexpr int kChunkWaves = 8, kChunkRows = 32 * kChunkWaves, kChunkKeys = 64;
 
 template <int D, int KDT>
@@ -802,14 +852,15 @@ struct ChunkGeom {
   static constexpr int kPerThread = 2 * kChunkKeys * kCpr / 512;      // 16-byte chunks of keys and values per thread
   static constexpr int kTile = kChunkKeys * D * 2;
   static constexpr int kBuffer = 2 * kTile + (KDT == 2 ? 2 * kChunkKeys * 4 : 0);
-  static constexpr int kLds = 2 * kBuffer + 32;
+  static constexpr int kLds = 2 * kBuffer + 8 * kChunkKeys * 12 + 8 * 8 + 8 * 4;
 };
 
 template <int D, int KDT>
 static __global__ __launch_bounds__(512, 2) void k_attn_chunk(AttnArgs a) {
   using Geo = ChunkGeom<D, KDT>;
   extern __shared__ __align__(16) unsigned char lds[];
-  const int lane = lane_id(), wave = threadIdx.x >> 6, half = lane >> 5, col = lane & 31;
+  const int lane = lane_id(), half = lane >> 5, col = lane & 31;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), group = wave >> 2;
 
   uint32_t id = blockIdx.x;
   const int hk = (int)(id % (uint32_t)a.H_kv);
@@ -817,7 +868,7 @@ static __global__ __launch_bounds__(512, 2) void k_attn_chunk(AttnArgs a) {
   const int split = (int)(id % (uint32_t)a.splits);
   const RowUnit u = find_unit<kChunkRows>(a, (int)(id / (uint32_t)a.splits));
   const int n = u.n, t_begin = u.t_begin, t_end = u.t_end;
-  const long r0 = u.r0, rows = (long)(t_end - t_begin) * a.G;
+  const int r0 = u.r0, rows = (t_end - t_begin) * a.G;
   if (r0 < 0 || r0 >= rows || t_begin < 0 || t_end > a.T) return;
   const int len = clamp_len(a, n);
   const int32_t* __restrict__ table = a.table + (long)n * a.max_pages;
@@ -825,8 +876,8 @@ static __global__ __launch_bounds__(512, 2) void k_attn_chunk(AttnArgs a) {
   // what the whole tile of rows sees, and what this wave's rows see
   int wg_pos = -1, wg_lo = 0x7fffffff, wg_pos_min = 0x7fffffff, wg_lo_max = 0;
   {
-    const long last = r0 + kChunkRows - 1 < rows - 1 ? r0 + kChunkRows - 1 : rows - 1;
-    for (int i = (int)(r0 / a.G) + lane; i <= (int)(last / a.G); i += 64) {
+    const int last = r0 + kChunkRows - 1 < rows - 1 ? r0 + kChunkRows - 1 : rows - 1;
+    for (int i = r0 / a.G + lane; i <= last / a.G; i += 64) {
       const Seen s = seen_by(a, n, len, t_begin + i, t_end);
       wg_pos = s.pos > wg_pos ? s.pos : wg_pos;
       wg_lo = s.lo < wg_lo ? s.lo : wg_lo;
@@ -839,11 +890,10 @@ static __global__ __launch_bounds__(512, 2) void k_attn_chunk(AttnArgs a) {
     wg_lo = wave_min_int(wg_lo);
   }
   RowState<D> st[1];
-  long r = r0 + wave * 32 + col;
+  int r = r0 + wave * 32 + col;
   const bool mine = r < rows;
-  const bool idle = r0 + wave * 32 >= rows;                  // no row of this wave is there
   if (!mine) r = rows - 1;
-  const int t = t_begin + (int)(r / a.G), h = hk * a.G + (int)(r % a.G);
+  const int t = t_begin + r / a.G, h = hk * a.G + r % a.G;
   st[0].clear();
   st[0].load_q((const uint16_t*)a.q + ((long)t * a.H + h) * D);
   {
@@ -851,8 +901,7 @@ static __global__ __launch_bounds__(512, 2) void k_attn_chunk(AttnArgs a) {
     st[0].pos = s.pos;
     st[0].lo = s.lo;
   }
-  const int pos_min = wave_min_int(st[0].pos), pos_max = wave_max_int(st[0].pos);
-  const int lo_min = wave_min_int(st[0].lo), lo_max = wave_max_int(st[0].lo);
+  const int pos_min = wave_min_int(st[0].pos), lo_max = wave_max_int(st[0].lo);
 
   int begin = wg_lo / kChunkKeys, end = (wg_pos + kChunkKeys) / kChunkKeys;
   if (wg_pos < 0 || end < begin) end = begin;
@@ -860,64 +909,70 @@ static __global__ __launch_bounds__(512, 2) void k_attn_chunk(AttnArgs a) {
     take_part(begin, end, split, a.splits, 4);
   }
 
-  // this thread's chunks of a tile: chunk x = i * 512 + thread, keys first, then values
-  constexpr int kHalf = kChunkKeys * Geo::kCpr;
+  // Wave 0 looks up where the rows of a tile lie, three tiles ahead, and leaves it in LDS for all: byte offsets (-1: nobody
+  // sees the row, or its page is none), fp8 slots, and a mask of the rows that are there; eight tiles of each.
   constexpr int kBytes = KDT == 2 ? 1 : 2;
-  auto row_of = [&](int i) { return ((i * 512 + (int)threadIdx.x) % kHalf) / Geo::kCpr; };
-  auto is_value = [&](int i) { return i * 512 + (int)threadIdx.x >= kHalf; };
-  auto page_of = [&](int tile, int row) {
-    const int s = tile * kChunkKeys + row;
-    return tile < end && s >= wg_lo && s <= wg_pos ? table[s >> a.page_shift] : -1;
+  long* offsets = reinterpret_cast<long*>(lds + 2 * Geo::kBuffer);                     // [8][64]
+  uint64_t* masks = reinterpret_cast<uint64_t*>(offsets + 8 * kChunkKeys);             // [8]
+  int* slots = reinterpret_cast<int*>(masks + 8);                                      // [8][64]
+  int* odd = slots + 8 * kChunkKeys;                                                   // [8]: tile with values dropped
+  if (threadIdx.x < 8) odd[threadIdx.x] = -1;
+  int page = -1;
+  auto lookup = [&](int tile) {
+    const int s = tile * kChunkKeys + lane;
+    page = tile < end && s >= wg_lo && s <= wg_pos ? table[s >> a.page_shift] : -1;
   };
-  int pages[Geo::kPerThread];
-  int scale_page = -1, mask_page = -1;
-  uint64_t there = 0;                      // rows of the tile in registers that are there
+  auto publish = [&](int tile) {
+    const int o = (tile * kChunkKeys + lane) & ((1 << a.page_shift) - 1);
+    const bool ok = (uint32_t)page < (uint32_t)a.n_pages;
+    const uint64_t mask = __builtin_amdgcn_ballot_w64(ok);
+    offsets[(tile & 7) * kChunkKeys + lane] = ok ? (page * a.page_stride + o * a.token_stride) * kBytes : -1;
+    if constexpr (KDT == 2) slots[(tile & 7) * kChunkKeys + lane] = ok ? (page << a.page_shift) + o : -1;
+    if (lane == 0) masks[tile & 7] = mask;
+  };
+
+  // this thread's chunks of a step: chunk x = i * 512 + thread, keys (of the next tile) first, then values
+  constexpr int kHalf = kChunkKeys * Geo::kCpr;
+  static_assert(kHalf == 256 || kHalf % 512 == 0, "keys and values meet between waves");
+  auto is_value = [&](int i) { return kHalf < 512 ? wave >= 4 : i * 512 >= kHalf; };
+  const int row0 = (kHalf < 512 ? (int)threadIdx.x % kHalf : (int)threadIdx.x) / Geo::kCpr;
+  auto row_of = [&](int i) { return row0 + (kHalf < 512 ? 0 : i * 512 % kHalf / Geo::kCpr); };
+  const unsigned char* __restrict__ kbase = (const unsigned char*)a.k + hk * a.head_stride * kBytes + threadIdx.x % Geo::kCpr * 16;
+  const unsigned char* __restrict__ vbase = (const unsigned char*)a.v + hk * a.head_stride * kBytes + threadIdx.x % Geo::kCpr * 16;
   uint4 x[Geo::kPerThread];
   float scale = 0.f;
-  auto lookup = [&](int tile) {
-#pragma unroll
-    for (int i = 0; i < Geo::kPerThread; ++i) pages[i] = page_of(tile, row_of(i));
-    mask_page = page_of(tile, lane);
-    if constexpr (KDT == 2) scale_page = threadIdx.x < 2 * kChunkKeys ? page_of(tile, threadIdx.x % kChunkKeys) : -1;
-  };
-  auto request = [&](int tile) {
-    there = __builtin_amdgcn_ballot_w64((uint32_t)mask_page < (uint32_t)a.n_pages);
+  auto request = [&](int step) {
+    // (a row that is none is read from the first row of the pool and cleared on its way into LDS: no branch holds the loads up)
+    const long *ka = offsets + ((step + 1) & 7) * kChunkKeys, *va = offsets + (step & 7) * kChunkKeys;
 #pragma unroll
     for (int i = 0; i < Geo::kPerThread; ++i) {
-      const int s = tile * kChunkKeys + row_of(i);
-      x[i] = make_uint4(0, 0, 0, 0);
-      if ((uint32_t)pages[i] < (uint32_t)a.n_pages) {
-        const long at = pages[i] * a.page_stride + (s & ((1 << a.page_shift) - 1)) * a.token_stride + hk * a.head_stride;
-        const unsigned char* src = (const unsigned char*)(is_value(i) ? a.v : a.k) + at * kBytes;
-        x[i] = *reinterpret_cast<const uint4*>(src + threadIdx.x % Geo::kCpr * 16);
-      }
+      const long off = (is_value(i) ? va : ka)[row_of(i)];
+      x[i] = *reinterpret_cast<const uint4*>((is_value(i) ? vbase : kbase) + (off < 0 ? 0 : off));
     }
     if constexpr (KDT == 2) {
-      const int s = tile * kChunkKeys + threadIdx.x % kChunkKeys;
       scale = 0.f;
-      if ((uint32_t)scale_page < (uint32_t)a.n_pages) {
-        const long slot = ((long)scale_page << a.page_shift) + (s & ((1 << a.page_shift) - 1));
-        scale = (threadIdx.x < kChunkKeys ? a.k_scale : a.v_scale)[slot * a.H_kv + hk];
+      if (threadIdx.x < 2 * kChunkKeys) {
+        const int slot = slots[((step + 1) & 7) * kChunkKeys + threadIdx.x % kChunkKeys];
+        if (slot >= 0) scale = (threadIdx.x < kChunkKeys ? a.k_scale : a.v_scale)[(long)slot * a.H_kv + hk];
       }
     }
   };
-  uint64_t* masks = reinterpret_cast<uint64_t*>(lds + 2 * Geo::kBuffer);     // of the two buffers
-  int* odd = reinterpret_cast<int*>(masks + 2);                               // tile with infinities or NaN dropped
-  if (threadIdx.x < 2) odd[threadIdx.x] = -1;
-  __syncthreads();
-  auto deposit = [&](int buffer, int tile) {
-    unsigned char* kt = lds + buffer * Geo::kBuffer;
-    unsigned char* vt = kt + Geo::kTile;
-    if (tile * kChunkKeys + kChunkKeys - 1 > wg_pos_min || tile * kChunkKeys < wg_lo_max) {
+  auto mixed = [&](int tile) { return tile * kChunkKeys + kChunkKeys - 1 > wg_pos_min || tile * kChunkKeys < wg_lo_max; };
+  auto deposit = [&](int step) {
+    unsigned char* kt = lds + ((step + 1) & 1) * Geo::kBuffer;
+    unsigned char* vt = lds + (step & 1) * Geo::kBuffer + Geo::kTile;
+    const uint64_t km = masks[(step + 1) & 7], vm = masks[step & 7];
+    if (__builtin_amdgcn_readfirstlane((int)(uint32_t)(km & vm) & (int)((km & vm) >> 32)) != -1) {
+#pragma unroll
+      for (int i = 0; i < Geo::kPerThread; ++i)
+        if (!((is_value(i) ? vm : km) >> row_of(i) & 1)) x[i] = make_uint4(0, 0, 0, 0);
+    }
+    if (mixed(step)) {
       bool found = false;
-      if (KDT == 2 && threadIdx.x >= kChunkKeys && !(__builtin_fabsf(scale) < __builtin_inff())) {
-        scale = 0.f;
-        found = true;
-      }
 #pragma unroll
       for (int i = 0; i < Geo::kPerThread; ++i)
         if (is_value(i)) found |= drop_odd<KDT>(x[i]);
-      if (found) odd[buffer] = tile;
+      if (found) odd[step & 7] = step;
     }
 #pragma unroll
     for (int i = 0; i < Geo::kPerThread; ++i) {
@@ -926,30 +981,48 @@ static __global__ __launch_bounds__(512, 2) void k_attn_chunk(AttnArgs a) {
       else store_chunk<D, KDT, false>(kt, row_of(i), c, x[i]);
     }
     if constexpr (KDT == 2)
-      if (threadIdx.x < 2 * kChunkKeys) reinterpret_cast<float*>(vt + Geo::kTile)[threadIdx.x] = scale;
-    if (threadIdx.x == 0) masks[buffer] = there;
+      if (threadIdx.x < 2 * kChunkKeys) {
+        if (threadIdx.x >= kChunkKeys && mixed(step + 1) && !(__builtin_fabsf(scale) < __builtin_inff())) {
+          scale = 0.f;
+          odd[(step + 1) & 7] = step + 1;
+        }
+        reinterpret_cast<float*>(kt + 2 * Geo::kTile)[threadIdx.x] = scale;
+      }
   };
 
   const int read_key = RowTile<D>::read_key(), read_value = RowTile<D>::read_value();
-  lookup(begin);
+  if (wave == 0) {
+    lookup(begin);
+    publish(begin);
+    lookup(begin + 1);
+    publish(begin + 1);
+    lookup(begin + 2);
+    publish(begin + 2);
+    lookup(begin + 3);
+    masks[(begin - 1) & 7] = 0;              // (step begin - 1 has keys and no values)
+    offsets[((begin - 1) & 7) * kChunkKeys + lane] = -1;
+  }
+  lds_barrier();
+  request(begin - 1);
+  deposit(begin - 1);
   request(begin);
-  lookup(begin + 1);
-  deposit(0, begin);
-  request(begin + 1);
-  lookup(begin + 2);
-  __syncthreads();
+  lds_barrier();
+  if (group == 1) {
+    deposit(begin);
+    request(begin + 1);
+    lds_barrier();
+  }
+  f32x16 s[1][2];
+  bf16x8 p[1][4];
+  score_tile<D, 2, 1>(st, lds + (begin & 1) * Geo::kBuffer, renewed(read_key), s);
   for (int tile = begin; tile < end; ++tile) {
-    const int buffer = (tile - begin) & 1;
-    const unsigned char* kt = lds + buffer * Geo::kBuffer;
-    const unsigned char* vt = kt + Geo::kTile;
-    const float* sc = reinterpret_cast<const float*>(vt + Geo::kTile);
     const int base = tile * kChunkKeys;
-    if (!idle && base <= pos_max && base + kChunkKeys - 1 >= lo_min) {
-      const uint64_t mask = masks[buffer];
-      const uint32_t keys[2] = {(uint32_t)mask, (uint32_t)(mask >> 32)};
-      f32x16 s[1][2];
-      bf16x8 p[1][4];
-      score_tile<D, 2, 1>(st, kt, renewed(read_key), s);
+    lds_barrier();
+    {
+      const float* sc = reinterpret_cast<const float*>(lds + (tile & 1) * Geo::kBuffer + 2 * Geo::kTile);
+      const uint64_t mask = masks[tile & 7];
+      const uint32_t keys[2] = {(uint32_t)__builtin_amdgcn_readfirstlane((int)mask),
+                                (uint32_t)__builtin_amdgcn_readfirstlane((int)(mask >> 32))};
       if constexpr (KDT == 2) scale_scores<2>(s[0], sc);
       if ((keys[0] & keys[1]) != 0xffffffffu || base + kChunkKeys - 1 > pos_min || base < lo_max) {
         asm volatile("");                  // (a branch, not 32 selects for every tile)
@@ -957,16 +1030,23 @@ static __global__ __launch_bounds__(512, 2) void k_attn_chunk(AttnArgs a) {
         hide(st[0], s[0][1], keys[1], base + 32);
       }
       softmax_tile<D, KDT, 2>(st[0], s[0], p[0], a.scale_log2, sc + kChunkKeys);
-      add_values<D, 2, 1>(st, vt, renewed(read_value), p);
-      if (odd[buffer] == tile) add_odd_values<D, KDT>(a, st[0], table, hk, base, kChunkKeys);
     }
-    if (tile + 1 < end) {
-      deposit(buffer ^ 1, tile + 1);
-      request(tile + 2);
-      lookup(tile + 3);
+    deposit(tile + group);
+    request(tile + group + 1);
+    if (wave == 0) {
+      publish(tile + 3);
+      lookup(tile + 4);
     }
-    __syncthreads();
+    lds_barrier();
+    // (behind the last tile there are keys of nobody, whose scores are not looked at)
+    const bool dropped = __builtin_amdgcn_readfirstlane(odd[tile & 7]) == tile;
+    products<D>(st[0], lds + ((tile + 1) & 1) * Geo::kBuffer, renewed(read_key), s[0],
+                lds + (tile & 1) * Geo::kBuffer + Geo::kTile, renewed(read_value), p[0]);
+    if (dropped)
+      add_odd_values<D, KDT>(st[0], (const unsigned char*)a.v + hk * a.head_stride * kBytes, offsets + (tile & 7) * kChunkKeys,
+                             slots + (tile & 7) * kChunkKeys, a.v_scale + hk, a.H_kv, base);
   }
+  if (group == 0) lds_barrier();
 
   if (!mine) return;
   const float l = add_halves(st[0].l);
