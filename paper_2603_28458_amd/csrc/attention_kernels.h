@@ -513,10 +513,11 @@ __device__ __forceinline__ void score_tile(const RowState<D> (&st)[NQ], const un
 // eight are under way from LDS while one is multiplied: the order is pinned, because the compiler's own asks for four at
 // most and the matrix unit then waits for LDS after every second product.  Consecutive products have different
 // accumulators.
-template <int D>
+template <int D, class Between>
 __device__ __forceinline__ void products(RowState<D>& st, const unsigned char* kt, int read_key, f32x16 (&s)[2],
-                                         const unsigned char* vt, int read_value, const bf16x8 (&p)[4]) {
-  constexpr int kAhead = 8, kScores = D / 8, kTiles = D / 32;
+                                         const unsigned char* vt, int read_value, const bf16x8 (&p)[4],
+                                         Between between) {
+  constexpr int kAhead = 6, kScores = D / 8, kTiles = D / 32;
   bf16x8 f[kAhead];
   auto operand = [&](int i) {
     return i < kScores ? RowTile<D>::key_operand(kt, read_key, 32 * (i & 1), i >> 1)
@@ -539,6 +540,7 @@ __device__ __forceinline__ void products(RowState<D>& st, const unsigned char* k
       st.o[j % kTiles] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, p[j / kTiles], st.o[j % kTiles], 0, 0, 0);
     }
     if (i + kAhead < 2 * kScores) f[i % kAhead] = operand(i + kAhead);
+    between(i);
     __builtin_amdgcn_sched_barrier(0);
   }
 }
@@ -833,27 +835,47 @@ static __global__ __launch_bounds__(256, NQ == 1 ? 2 : 1) void k_attn_rows(AttnA
 
 // ---- many rows per sequence ----------------------------------------------------------------------
 // A workgroup of 8 waves takes 256 query rows of one KV head (32 per wave) and a part of their keys, in tiles of 64 keys
-// that all waves multiply from LDS (two buffers for keys and for values).  Bound by the matrix units (4 D flop per visible
-// pair).  Each SIMD holds two waves, one of the first four and one of the last four, half a tile apart: in every phase,
-// between two barriers, one of them runs its products (scores of tile i, values of tile i - 1) while the other turns its
-// scores into weights and moves its share of the next rows from registers to LDS.  Running together, both would wait for
-// the matrix unit first and leave it idle afterwards.
+// that all waves multiply from LDS.  Bound by the matrix units (4 D flop per visible pair).  Each SIMD holds two waves, one
+// of the first four (group 0) and one of the last four (group 1).  In interval i, between two barriers, group 0 turns its
+// scores of tile i into weights, then runs its products for tile i + 1 (scores of tile i + 1, values of tile i), while
+// group 1 runs its products for tile i, then turns those scores into weights: one computes while the other multiplies, and
+// neither waits for the other half way.  Keys of tile i are thus read in intervals i - 1 (group 0) and i (group 1), values
+// of tile i in intervals i and i + 1.
 //
-// Phase 2 i + g is the products of group g for tile i, phase 2 i + 1 + g its softmax.  Keys of tile i are read in phases
-// 2 i and 2 i + 1, values of tile i in phases 2 i + 2 and 2 i + 3.  Step i (keys of tile i + 1, values of tile i, written in
-// phases 2 i and 2 i + 1: by the last four waves in the softmax phase of tile i - 1, by the first four in that of tile i)
-// therefore finds its buffers unread.  Scales go with the keys and are read in phases 2 i + 1 and 2 i + 2 by the softmax;
-// waves 0 and 1 alone write them, in phase 2 i + 1 of step i, when those of tile i - 1, in the same buffer, are done with.
+// Rows go from memory to LDS without passing registers (there are none left to hold a tile that is under way for as long as
+// HBM takes).  What is asked for in one interval has arrived when the next one ends.
+//   bf16  interval i asks for keys of tile i + 3 and values of tile i + 2, into four buffers each, in their final places:
+//         keys of tile i - 1 were last read in interval i - 1, values of tile i - 2 as well.
+//   fp8   interval i asks for keys of tile i + 4 and values of tile i + 3, as stored, into three buffers in which a thread
+//         finds its own 16 bytes again; in interval i + 2 it widens them into three tile buffers: keys of tile i + 4 take
+//         that of tile i + 1, last read in interval i + 1, values of tile i + 3 that of tile i, last read there too.
+// The requests are written as instructions of their own, and waited for by count: from its own builtins the compiler would
+// wait for all of them before every read of LDS.
 constexpr int kChunkWaves = 8, kChunkRows = 32 * kChunkWaves, kChunkKeys = 64;
 
 template <int D, int KDT>
 struct ChunkGeom {
-  static constexpr int kCpr = D * (KDT == 2 ? 1 : 2) / 16;
-  static constexpr int kPerThread = 2 * kChunkKeys * kCpr / 512;      // 16-byte chunks of keys and values per thread
+  static constexpr int kCpr = D * (KDT == 2 ? 1 : 2) / 16;            // stored 16-byte chunks of a row
+  static constexpr int kPerThread = 2 * kChunkKeys * kCpr / 512;      // of keys and values per thread and step
   static constexpr int kTile = kChunkKeys * D * 2;
-  static constexpr int kBuffer = 2 * kTile + (KDT == 2 ? 2 * kChunkKeys * 4 : 0);
-  static constexpr int kLds = 2 * kBuffer + 8 * kChunkKeys * 12 + 8 * 8 + 8 * 4;
+  static constexpr int kBuffers = KDT == 2 ? 3 : 4;
+  static constexpr int kRaw = 2 * kChunkKeys * kCpr * 16;             // stored bytes of a step
+  static constexpr int kRings = kBuffers * 2 * kTile + (KDT == 2 ? 3 * kRaw : 0);
+  // and: offsets [8][64] of 8 bytes, masks [8] of 8, pages [8][64] and slots [8][64] of 4, odd [8], scales [8][2][64] (fp8)
+  static constexpr int kLds = kRings + 8 * kChunkKeys * 16 + 8 * 8 + 8 * 4 + (KDT == 2 ? 8 * 2 * kChunkKeys * 4 : 0);
 };
+
+// 16 or 4 bytes per lane from `src` to LDS byte lds + 16 (or 4) * lane.
+__device__ __forceinline__ void dma16(uint32_t lds, const void* src) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds), "v"(src) : "memory", "m0");
+}
+__device__ __forceinline__ void dma4(uint32_t lds, const void* src) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(lds), "v"(src) : "memory", "m0");
+}
+template <int N>
+__device__ __forceinline__ void dma_left() {   // until at most N requests of this wave are under way
+  asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
+}
 
 template <int D, int KDT>
 static __global__ __launch_bounds__(512, 2) void k_attn_chunk(AttnArgs a) {
@@ -890,10 +912,10 @@ static __global__ __launch_bounds__(512, 2) void k_attn_chunk(AttnArgs a) {
     wg_lo = wave_min_int(wg_lo);
   }
   RowState<D> st[1];
-  int r = r0 + wave * 32 + col;
-  const bool mine = r < rows;
-  if (!mine) r = rows - 1;
-  const int t = t_begin + r / a.G, h = hk * a.G + r % a.G;
+  int qr = r0 + wave * 32 + col;
+  const bool mine = qr < rows;
+  if (!mine) qr = rows - 1;
+  const int t = t_begin + qr / a.G, h = hk * a.G + qr % a.G;
   st[0].clear();
   st[0].load_q((const uint16_t*)a.q + ((long)t * a.H + h) * D);
   {
@@ -909,144 +931,217 @@ static __global__ __launch_bounds__(512, 2) void k_attn_chunk(AttnArgs a) {
     take_part(begin, end, split, a.splits, 4);
   }
 
-  // Wave 0 looks up where the rows of a tile lie, three tiles ahead, and leaves it in LDS for all: byte offsets (-1: nobody
+  // Wave 0 finds out where the rows of a tile lie, five tiles ahead, and leaves it in LDS for all: byte offsets (-1: nobody
   // sees the row, or its page is none), fp8 slots, and a mask of the rows that are there; eight tiles of each.
   constexpr int kBytes = KDT == 2 ? 1 : 2;
-  long* offsets = reinterpret_cast<long*>(lds + 2 * Geo::kBuffer);                     // [8][64]
+  long* offsets = reinterpret_cast<long*>(lds + Geo::kRings);                          // [8][64]
   uint64_t* masks = reinterpret_cast<uint64_t*>(offsets + 8 * kChunkKeys);             // [8]
-  int* slots = reinterpret_cast<int*>(masks + 8);                                      // [8][64]
+  int* pages = reinterpret_cast<int*>(masks + 8);                                      // [8][64]
+  int* slots = pages + 8 * kChunkKeys;                                                 // [8][64]
   int* odd = slots + 8 * kChunkKeys;                                                   // [8]: tile with values dropped
+  float* scales = reinterpret_cast<float*>(odd + 8);                                   // [8][2][64] (fp8)
   if (threadIdx.x < 8) odd[threadIdx.x] = -1;
-  int page = -1;
-  auto lookup = [&](int tile) {
+  auto seen_row = [&](int tile) {            // of this lane
     const int s = tile * kChunkKeys + lane;
-    page = tile < end && s >= wg_lo && s <= wg_pos ? table[s >> a.page_shift] : -1;
+    return tile < end && s >= wg_lo && s <= wg_pos;
   };
-  auto publish = [&](int tile) {
+  auto page_entry = [&](int tile) {          // (an entry that there is, whatever the tile)
+    return table + (seen_row(tile) ? (tile * kChunkKeys + lane) >> a.page_shift : 0);
+  };
+  auto publish = [&](int tile, int page) {
     const int o = (tile * kChunkKeys + lane) & ((1 << a.page_shift) - 1);
-    const bool ok = (uint32_t)page < (uint32_t)a.n_pages;
+    const bool ok = seen_row(tile) && (uint32_t)page < (uint32_t)a.n_pages;
     const uint64_t mask = __builtin_amdgcn_ballot_w64(ok);
     offsets[(tile & 7) * kChunkKeys + lane] = ok ? (page * a.page_stride + o * a.token_stride) * kBytes : -1;
     if constexpr (KDT == 2) slots[(tile & 7) * kChunkKeys + lane] = ok ? (page << a.page_shift) + o : -1;
     if (lane == 0) masks[tile & 7] = mask;
   };
+  auto mask_of = [&](int tile) {
+    const uint64_t m = masks[tile & 7];
+    return (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(m >> 32)) << 32 |
+           (uint32_t)__builtin_amdgcn_readfirstlane((int)m);
+  };
 
-  // this thread's chunks of a step: chunk x = i * 512 + thread, keys (of the next tile) first, then values
+  // this thread's chunks of a step (keys of one tile and values of the tile before it): chunk i * 512 + thread, keys first
   constexpr int kHalf = kChunkKeys * Geo::kCpr;
   static_assert(kHalf == 256 || kHalf % 512 == 0, "keys and values meet between waves");
   auto is_value = [&](int i) { return kHalf < 512 ? wave >= 4 : i * 512 >= kHalf; };
   const int row0 = (kHalf < 512 ? (int)threadIdx.x % kHalf : (int)threadIdx.x) / Geo::kCpr;
   auto row_of = [&](int i) { return row0 + (kHalf < 512 ? 0 : i * 512 % kHalf / Geo::kCpr); };
-  const unsigned char* __restrict__ kbase = (const unsigned char*)a.k + hk * a.head_stride * kBytes + threadIdx.x % Geo::kCpr * 16;
-  const unsigned char* __restrict__ vbase = (const unsigned char*)a.v + hk * a.head_stride * kBytes + threadIdx.x % Geo::kCpr * 16;
-  uint4 x[Geo::kPerThread];
-  float scale = 0.f;
-  auto request = [&](int step) {
-    // (a row that is none is read from the first row of the pool and cleared on its way into LDS: no branch holds the loads up)
-    const long *ka = offsets + ((step + 1) & 7) * kChunkKeys, *va = offsets + (step & 7) * kChunkKeys;
+  // bf16: the chunk of a row that lies at this thread's place of a tile
+  const int col0 = threadIdx.x % Geo::kCpr;
+  const int kcol = KDT == 2 ? col0 : RowTile<D>::key_byte(row0, col0) / 16 % Geo::kCpr;
+  const int vcol = KDT == 2 ? col0 : RowTile<D>::value_byte(row0, col0) / 16 % Geo::kCpr;
+  const unsigned char* __restrict__ kbase = (const unsigned char*)a.k + hk * a.head_stride * kBytes + kcol * 16;
+  const unsigned char* __restrict__ vbase = (const unsigned char*)a.v + hk * a.head_stride * kBytes + vcol * 16;
+  const uint32_t lds0 = lds_address(lds);
+  // buffer of a tile: its number modulo four (bf16), or modulo three, counted from `begin` on (fp8)
+  auto after = [](int r) { return KDT == 2 ? (r == 2 ? 0 : r + 1) : (r + 1) & 3; };
+  auto before = [](int r) { return KDT == 2 ? (r == 0 ? 2 : r - 1) : (r + 3) & 3; };
+  auto key_tile = [&](int ring) { return ring * 2 * Geo::kTile; };
+  auto value_tile = [&](int ring) { return ring * 2 * Geo::kTile + Geo::kTile; };
+  constexpr int kRawAt = Geo::kBuffers * 2 * Geo::kTile;
+  // byte of chunk i (its wave's first) of the step with the keys of the tile of buffer r; fp8: in the raw buffer
+  auto place = [&](int i, int r) {
+    if (KDT == 2) return kRawAt + r * Geo::kRaw + (i * 512 + wave * 64) * 16;
+    return is_value(i) ? value_tile(before(r)) + (i * 512 - kHalf + wave * 64) * 16 : key_tile(r) + (i * 512 + wave * 64) * 16;
+  };
+  struct Where {
+    long at[Geo::kPerThread];
+    int slot;
+  };
+  auto where = [&](int tile) {              // of the step with the keys of `tile`
+    Where w;
 #pragma unroll
-    for (int i = 0; i < Geo::kPerThread; ++i) {
-      const long off = (is_value(i) ? va : ka)[row_of(i)];
-      x[i] = *reinterpret_cast<const uint4*>((is_value(i) ? vbase : kbase) + (off < 0 ? 0 : off));
-    }
-    if constexpr (KDT == 2) {
-      scale = 0.f;
-      if (threadIdx.x < 2 * kChunkKeys) {
-        const int slot = slots[((step + 1) & 7) * kChunkKeys + threadIdx.x % kChunkKeys];
-        if (slot >= 0) scale = (threadIdx.x < kChunkKeys ? a.k_scale : a.v_scale)[(long)slot * a.H_kv + hk];
-      }
-    }
+    for (int i = 0; i < Geo::kPerThread; ++i)
+      w.at[i] = offsets[((tile - is_value(i)) & 7) * kChunkKeys + row_of(i)];
+    if constexpr (KDT == 2) w.slot = slots[(tile & 7) * kChunkKeys + lane];
+    return w;
+  };
+  // (a row that is none is read from the first row of the pool, and cleared once it is there)
+  auto request = [&](int tile, const Where& w, int r, int page_tile) {
+    if (wave == 0) dma4(lds0 + (uint32_t)((unsigned char*)(pages + (page_tile & 7) * kChunkKeys) - lds), page_entry(page_tile));
+    if (KDT == 2 && wave < 2)
+      dma4(lds0 + (uint32_t)((unsigned char*)(scales + ((tile & 7) * 2 + wave) * kChunkKeys) - lds),
+           (wave == 0 ? a.k_scale : a.v_scale) + (long)(w.slot < 0 ? 0 : w.slot) * a.H_kv + hk);
+#pragma unroll
+    for (int i = 0; i < Geo::kPerThread; ++i)
+      dma16(lds0 + place(i, r), (is_value(i) ? vbase : kbase) + (w.at[i] < 0 ? 0 : w.at[i]));
+  };
+  auto step_arrived = [&]() {               // the step before the last one that was requested
+    constexpr int n = Geo::kPerThread + (KDT == 2);
+    if (wave == 0) dma_left<n + 1>();
+    else if (wave == 1) dma_left<n>();
+    else dma_left<Geo::kPerThread>();
   };
   auto mixed = [&](int tile) { return tile * kChunkKeys + kChunkKeys - 1 > wg_pos_min || tile * kChunkKeys < wg_lo_max; };
-  auto deposit = [&](int step) {
-    unsigned char* kt = lds + ((step + 1) & 1) * Geo::kBuffer;
-    unsigned char* vt = lds + (step & 1) * Geo::kBuffer + Geo::kTile;
-    const uint64_t km = masks[(step + 1) & 7], vm = masks[step & 7];
-    if (__builtin_amdgcn_readfirstlane((int)(uint32_t)(km & vm) & (int)((km & vm) >> 32)) != -1) {
+  // chunk i of an arrived step: cleared where its row is none, and of infinities and NaN in a mixed tile
+  auto cleaned = [&](int i, uint4 x, uint64_t km, uint64_t vm, int tile) {
+    if (!((is_value(i) ? vm : km) >> row_of(i) & 1)) x = make_uint4(0, 0, 0, 0);
+    if (is_value(i) && mixed(tile - 1) && drop_odd<KDT>(x)) odd[(tile - 1) & 7] = tile - 1;
+    return x;
+  };
+  // What an arrived step (keys of `tile`, in buffer r) still needs: bf16 only where there is something to clean, fp8 to be
+  // widened, from raw buffer `raw`.
+  auto finish = [&](int tile, int r, int raw, uint64_t km, uint64_t vm) {
+    const bool clean = (km & vm) != ~0ull || mixed(tile - 1);
+    if constexpr (KDT == 1) {
+      if (clean) {
 #pragma unroll
-      for (int i = 0; i < Geo::kPerThread; ++i)
-        if (!((is_value(i) ? vm : km) >> row_of(i) & 1)) x[i] = make_uint4(0, 0, 0, 0);
-    }
-    if (mixed(step)) {
-      bool found = false;
-#pragma unroll
-      for (int i = 0; i < Geo::kPerThread; ++i)
-        if (is_value(i)) found |= drop_odd<KDT>(x[i]);
-      if (found) odd[step & 7] = step;
-    }
-#pragma unroll
-    for (int i = 0; i < Geo::kPerThread; ++i) {
-      const int c = threadIdx.x % Geo::kCpr;
-      if (is_value(i)) store_chunk<D, KDT, true>(vt, row_of(i), c, x[i]);
-      else store_chunk<D, KDT, false>(kt, row_of(i), c, x[i]);
-    }
-    if constexpr (KDT == 2)
-      if (threadIdx.x < 2 * kChunkKeys) {
-        if (threadIdx.x >= kChunkKeys && mixed(step + 1) && !(__builtin_fabsf(scale) < __builtin_inff())) {
-          scale = 0.f;
-          odd[(step + 1) & 7] = step + 1;
+        for (int i = 0; i < Geo::kPerThread; ++i) {
+          uint4* p = reinterpret_cast<uint4*>(lds + place(i, r)) + lane;
+          *p = cleaned(i, *p, km, vm, tile);
         }
-        reinterpret_cast<float*>(kt + 2 * Geo::kTile)[threadIdx.x] = scale;
       }
+    } else {
+      if (wave == 1) {
+        float* sc = scales + ((tile & 7) * 2 + 1) * kChunkKeys + lane;
+        if (!(km >> lane & 1)) *sc = 0.f;
+        else if (mixed(tile) && !(__builtin_fabsf(*sc) < __builtin_inff())) {
+          *sc = 0.f;
+          odd[tile & 7] = tile;
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < Geo::kPerThread; ++i) {
+        uint4 x = reinterpret_cast<const uint4*>(lds + place(i, raw))[lane];
+        if (clean) x = cleaned(i, x, km, vm, tile);
+        if (is_value(i)) store_chunk<D, 2, true>(lds + value_tile(before(r)), row_of(i), col0, x);
+        else store_chunk<D, 2, false>(lds + key_tile(r), row_of(i), col0, x);
+      }
+    }
   };
 
   const int read_key = RowTile<D>::read_key(), read_value = RowTile<D>::read_value();
   if (wave == 0) {
-    lookup(begin);
-    publish(begin);
-    lookup(begin + 1);
-    publish(begin + 1);
-    lookup(begin + 2);
-    publish(begin + 2);
-    lookup(begin + 3);
-    masks[(begin - 1) & 7] = 0;              // (step begin - 1 has keys and no values)
+    int first[6];
+#pragma unroll
+    for (int i = 0; i < 6; ++i) first[i] = *page_entry(begin + i);
+#pragma unroll
+    for (int i = 0; i < 5; ++i) publish(begin + i, first[i]);
+    pages[((begin + 5) & 7) * kChunkKeys + lane] = first[5];
+    masks[(begin - 1) & 7] = 0;              // (the first step has keys and no values)
     offsets[((begin - 1) & 7) * kChunkKeys + lane] = -1;
   }
   lds_barrier();
-  request(begin - 1);
-  deposit(begin - 1);
-  request(begin);
+  // r: buffer of the present tile; fp8: raw buffer of the step that is widened for the next one
+  int r = KDT == 2 ? 0 : begin & 3;
+  request(begin, where(begin), r, begin + 6);
+  request(begin + 1, where(begin + 1), after(r), begin + 6);
+  if constexpr (KDT == 2) request(begin + 2, where(begin + 2), after(after(r)), begin + 6);
+  dma_left<0>();
+  finish(begin, r, r, mask_of(begin), 0);
+  finish(begin + 1, after(r), after(r), mask_of(begin + 1), mask_of(begin));
+  if (group == 1) request(begin + 2 + (KDT == 2), where(begin + 2 + (KDT == 2)), KDT == 2 ? r : after(after(r)), 0);
   lds_barrier();
-  if (group == 1) {
-    deposit(begin);
-    request(begin + 1);
-    lds_barrier();
-  }
   f32x16 s[1][2];
   bf16x8 p[1][4];
-  score_tile<D, 2, 1>(st, lds + (begin & 1) * Geo::kBuffer, renewed(read_key), s);
+  if (group == 1) lds_barrier();
+  score_tile<D, 2, 1>(st, lds + key_tile(r), renewed(read_key), s);
+  {
+    // (fp8: what group 1 widens here, and group 0 between the products for the next tile, came with the third request)
+    const int tile = begin + group;
+    const Where at = where(tile + 2 + (KDT == 2));
+    if (KDT == 2 && group == 1) finish(begin + 2, after(after(r)), after(after(r)), mask_of(begin + 2), mask_of(begin + 1));
+    const int to = KDT == 2 ? (group == 1 ? after(r) : r) : (tile + 2) & 3;
+    request(tile + 2 + (KDT == 2), at, to, begin + 6 + (KDT == 2));
+  }
+  if (group == 0) lds_barrier();
   for (int tile = begin; tile < end; ++tile) {
-    const int base = tile * kChunkKeys;
-    lds_barrier();
+    const int base = tile * kChunkKeys, r1 = after(r), r2 = after(r1);
+    const uint64_t mask = mask_of(tile), km = mask_of(tile + 2), vm = mask_of(tile + 1);
     {
-      const float* sc = reinterpret_cast<const float*>(lds + (tile & 1) * Geo::kBuffer + 2 * Geo::kTile);
-      const uint64_t mask = masks[tile & 7];
-      const uint32_t keys[2] = {(uint32_t)__builtin_amdgcn_readfirstlane((int)mask),
-                                (uint32_t)__builtin_amdgcn_readfirstlane((int)(mask >> 32))};
+      const float* sc = scales + (tile & 7) * 2 * kChunkKeys;
       if constexpr (KDT == 2) scale_scores<2>(s[0], sc);
-      if ((keys[0] & keys[1]) != 0xffffffffu || base + kChunkKeys - 1 > pos_min || base < lo_max) {
+      if (mask != ~0ull || base + kChunkKeys - 1 > pos_min || base < lo_max) {
         asm volatile("");                  // (a branch, not 32 selects for every tile)
-        hide(st[0], s[0][0], keys[0], base);
-        hide(st[0], s[0][1], keys[1], base + 32);
+        hide(st[0], s[0][0], (uint32_t)mask, base);
+        hide(st[0], s[0][1], (uint32_t)(mask >> 32), base + 32);
       }
       softmax_tile<D, KDT, 2>(st[0], s[0], p[0], a.scale_log2, sc + kChunkKeys);
     }
-    deposit(tile + group);
-    request(tile + group + 1);
-    if (wave == 0) {
-      publish(tile + 3);
-      lookup(tile + 4);
+    // (the weights are made here and not, as the compiler would have it, between the products that need them)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) asm volatile("" : "+v"(p[0][i]));
+    asm volatile("" : "+v"(st[0].l));
+    if (wave == 0) publish(tile + 5, pages[((tile + 5) & 7) * kChunkKeys + lane]);
+    if (group == 1) {
+      if constexpr (KDT == 1) {
+        step_arrived();
+        finish(tile + 2, r2, 0, km, vm);
+      }
+      lds_barrier();
     }
-    lds_barrier();
-    // (behind the last tile there are keys of nobody, whose scores are not looked at)
+    // products for the next tile (behind the last one there are keys of nobody, whose scores are not looked at)
+    __builtin_amdgcn_sched_barrier(0);
     const bool dropped = __builtin_amdgcn_readfirstlane(odd[tile & 7]) == tile;
-    products<D>(st[0], lds + ((tile + 1) & 1) * Geo::kBuffer, renewed(read_key), s[0],
-                lds + (tile & 1) * Geo::kBuffer + Geo::kTile, renewed(read_value), p[0]);
+    const int asked = tile + 3 + group + (KDT == 2);
+    if constexpr (KDT == 2) {
+      // group 0 is in interval `tile`, group 1 in the next one: keys of tile + 2, of tile + 3
+      step_arrived();
+      if (group == 0) finish(tile + 2, r2, r2, km, vm);
+      else finish(tile + 3, r, r, mask_of(tile + 3), km);
+    }
+    Where at;
+    constexpr int kProducts = D / 4;
+    products<D>(st[0], lds + key_tile(r1), renewed(read_key), s[0], lds + value_tile(r), renewed(read_value), p[0], [&](int i) {
+      if (i == 1) at = where(asked);
+      // (fp8: the buffer of the step before the one that is widened now)
+      if (i == kProducts / 4) request(asked, at, KDT == 2 ? (group == 0 ? r1 : r2) : asked & 3, tile + 7 + (KDT == 2));
+    });
     if (dropped)
       add_odd_values<D, KDT>(st[0], (const unsigned char*)a.v + hk * a.head_stride * kBytes, offsets + (tile & 7) * kChunkKeys,
                              slots + (tile & 7) * kChunkKeys, a.v_scale + hk, a.H_kv, base);
+    if (group == 0) {
+      if constexpr (KDT == 1) {
+        step_arrived();
+        finish(tile + 2, r2, 0, km, vm);
+      }
+      lds_barrier();
+    }
+    r = r1;
   }
-  if (group == 0) lds_barrier();
+  dma_left<0>();                           // (LDS is somebody else's once the workgroup has ended)
 
   if (!mine) return;
   const float l = add_halves(st[0].l);
