@@ -3,6 +3,8 @@
 // x = log2(e) * scale * (q . k); parts of a row are joined by the same rule.
 #pragma once
 
+#include <utility>
+
 #include "hisa_device.h"
 
 namespace hisa {
@@ -29,6 +31,12 @@ struct AttnArgs {
   int n_pages, page_shift, n_seq, max_pages;
   int splits;
 };
+
+// f(0), f(1), .. f(N - 1) with the number as a type: a loop that is written out whatever its size.
+template <class F, int... I>
+__device__ __forceinline__ void steps(F&& f, std::integer_sequence<int, I...>) {
+  (f(std::integral_constant<int, I>{}), ...);
+}
 
 // Last n in [0, n_seq) for which `le(n)` holds (ascending: true up to it), by the whole wave, 64 candidates at a time; 0 if
 // it holds for none.
@@ -621,46 +629,57 @@ __device__ __forceinline__ void store_result(const AttnArgs& a, int split, long 
 }
 
 // ---- one token at a time, over a range or a list: keys split over the waves -----------------------
-// A workgroup of 4 waves takes one token, up to NQ * 32 heads of one KV head's group and a part of the keys.  Every wave
-// works alone on its own tiles of 32 keys (every fourth): the next tile's rows are on their way into registers while the
-// present one, in the wave's own 32 * D * 4 bytes of LDS, is multiplied; the waves' results are joined at the end.  All
-// rows see the same keys, so a row outside is a row of zeros and a score of -inf for everybody.  Bound by memory: 4 D
-// bytes (bf16) per key and KV head, whatever the number of heads.
+// A workgroup takes one token, up to 32 heads of one KV head's group (64: PAIR) and a part of the keys.  Each of 4 waves
+// works alone on its own tiles of 32 keys (every fourth): later tiles' rows are on their way into registers while the
+// present one, in the wave's own LDS, is multiplied; the waves' results are joined at the end.  With PAIR a wave has a
+// second one beside it on its SIMD: one brings the keys of their tile, the other the values, and each multiplies 32 of the
+// heads, so that wider groups gather every row once and still leave each SIMD two waves.  All rows see the same keys, so a
+// row outside is a row of zeros and a score of -inf for everybody.  Bound by memory: 4 D bytes (bf16) per key and KV head,
+// whatever the number of heads.
 constexpr int kRowWaves = 4;
 
-template <int D, int KDT>
+template <int D, int KDT, bool PAIR>
 struct RowGeom {
   static constexpr int kCpr = D * (KDT == 2 ? 1 : 2) / 16;   // stored 16-byte chunks of a row
   static constexpr int kRpi = 64 / kCpr;                     // rows per load instruction
   static constexpr int kNi = 32 / kRpi;                      // load instructions per 32 rows
+  static constexpr int kLoads = PAIR ? kNi : 2 * kNi;        // of a wave per tile
+  static constexpr int kDepth = PAIR || KDT == 2 || D == 64 ? 2 : 1;   // tiles under way: two where the registers allow it
   static constexpr int kTile = 32 * D * 2;                   // LDS bytes of 32 keys, or values
-  static constexpr int kWaveLds = 2 * kTile + (KDT == 2 ? 256 : 0);
-  static constexpr int kLds = kRowWaves * kWaveLds + kRowWaves * 32 * 8;
+  static constexpr int kStage = 2 * kTile + (KDT == 2 ? 256 : 0);
+  static constexpr int kStages = PAIR ? 2 : 1;
+  static constexpr int kWaves = PAIR ? 2 * kRowWaves : kRowWaves;
+  // rings, then per wave 32 row offsets, then per wave (m, l) of 32 rows
+  static constexpr int kOffsets = kRowWaves * kStages * kStage, kJoin = kOffsets + kWaves * 256;
+  static constexpr int kLds = kJoin + kWaves * 256;
 };
 
-template <int D, int KDT, int NQ, bool LIST>
-static __global__ __launch_bounds__(256, NQ == 1 ? 2 : 1) void k_attn_rows(AttnArgs a) {
-  using Geo = RowGeom<D, KDT>;
+template <int D, int KDT, bool PAIR, bool LIST>
+static __global__ __launch_bounds__(PAIR ? 512 : 256, 2) void k_attn_rows(AttnArgs a) {
+  using Geo = RowGeom<D, KDT, PAIR>;
   extern __shared__ __align__(16) unsigned char lds[];
-  const int lane = lane_id(), wave = threadIdx.x >> 6, half = lane >> 5, col = lane & 31;
-  unsigned char* kt = lds + wave * Geo::kWaveLds;
-  unsigned char* vt = kt + Geo::kTile;
-  float* sc = reinterpret_cast<float*>(vt + Geo::kTile);                       // 32 key scales, 32 value scales
-  float* join = reinterpret_cast<float*>(lds + kRowWaves * Geo::kWaveLds);     // [wave][32][2]
+  const int lane = lane_id(), half = lane >> 5, col = lane & 31;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lead = wave & 3, second = PAIR ? wave >> 2 : 0;
+  unsigned char* ring = lds + lead * Geo::kStages * Geo::kStage;
+  long* row_at = reinterpret_cast<long*>(lds + Geo::kOffsets) + wave * 32;
+  float* join = reinterpret_cast<float*>(lds + Geo::kJoin);                    // [wave][32][2]
 
   uint32_t id = blockIdx.x;
   const int hk = (int)(id % (uint32_t)a.H_kv);
   id /= (uint32_t)a.H_kv;
   const int split = (int)(id % (uint32_t)a.splits);
   const int unit = (int)(id / (uint32_t)a.splits);
-  const int head_tiles = (a.G + 32 * NQ - 1) / (32 * NQ);
-  const int t = unit / head_tiles, r0 = (unit - t * head_tiles) * 32 * NQ;
-  int n, len, lo = 0, pos = 0;
+  constexpr int kHeads = PAIR ? 64 : 32;
+  const int head_tiles = (a.G + kHeads - 1) / kHeads;
+  const int t = unit / head_tiles, r0 = (unit - t * head_tiles) * kHeads + second * 32;
+  int n, len, lo = 0, pos = 0, begin, end;      // tiles of 32 keys (list entries); range tiles begin at multiples of 32
   if constexpr (LIST) {
     n = a.q_seq ? a.q_seq[t] : 0;
     const bool none = (uint32_t)n >= (uint32_t)a.n_seq;
     n = none ? 0 : n;
     len = none ? 0 : clamp_len(a, n);
+    begin = 0;
+    end = (a.n_list + 31) / 32;
   } else {
     n = last_seq(a.n_seq, [&](int i) { return a.q_start[i] <= t; });
     const int t_end = a.q_start[n + 1];
@@ -669,166 +688,190 @@ static __global__ __launch_bounds__(256, NQ == 1 ? 2 : 1) void k_attn_rows(AttnA
     const Seen s = seen_by(a, n, len, t, t_end);
     lo = s.lo;
     pos = s.pos;
-  }
-  const int32_t* __restrict__ table = a.table + (long)n * a.max_pages;
-  RowState<D> st[NQ];
-#pragma unroll
-  for (int q = 0; q < NQ; ++q) {          // (columns beyond the last head repeat it and are not stored)
-    int r = r0 + q * 32 + col;
-    if (r >= a.G) r = a.G - 1;
-    st[q].clear();
-    st[q].load_q((const uint16_t*)a.q + ((long)t * a.H + hk * a.G + r) * D);
-  }
-  int begin, end;                         // tiles of 32 keys (list entries); range tiles begin at multiples of 32
-  if constexpr (LIST) {
-    begin = 0;
-    end = len > 0 ? (a.n_list + 31) / 32 : 0;
-  } else {
     begin = lo >> 5;
     end = (pos + 32) >> 5;
     if (pos < 0 || end < begin) end = begin;
   }
-  if (a.splits > 1) {
-    take_part(begin, end, split, a.splits, 8);      // of at least two tiles per wave
-  }
+  if (a.splits > 1) take_part(begin, end, split, a.splits, 8);      // of at least two tiles per wave
+  const int32_t* __restrict__ table = a.table + (long)n * a.max_pages;
+  const int cap_last = (int)(((long)a.max_pages << a.page_shift) - 1);
 
-  // page lookups run two tiles ahead of the rows, list entries three
-  auto position = [&](int tile) {         // of key `col` of a tile, or -1
+  // position of key `col` of a tile (or one that is no position), and the table's entry for it, whatever it is
+  auto position = [&](int tile) {
     if (tile >= end) return -1;
     const int c = tile * 32 + col;
     if constexpr (LIST) return c < a.n_list ? a.list[(long)t * a.n_list + c] : -1;
     else return c;
   };
   auto page_of = [&](int s) {
-    const bool ok = LIST ? s >= 0 && s < len : s >= lo && s <= pos;
-    return ok ? table[s >> a.page_shift] : -1;
+    const int in = s < 0 ? 0 : s > cap_last ? cap_last : s;
+    return table[in >> a.page_shift];
+  };
+  auto counts = [&](int s, int page) {
+    const bool seen = LIST ? s >= 0 && s < len : s >= lo && s <= pos;
+    return seen && (uint32_t)page < (uint32_t)a.n_pages;
   };
   constexpr int kBytes = KDT == 2 ? 1 : 2;
-  const unsigned char* __restrict__ kbase = (const unsigned char*)a.k + hk * a.head_stride * kBytes;
-  const unsigned char* __restrict__ vbase = (const unsigned char*)a.v + hk * a.head_stride * kBytes;
-  uint4 kr[Geo::kNi], vr[Geo::kNi];
-  float scale = 0.f;
-  uint32_t valid = 0;                     // rows of the tile in registers that there are
-  // a tile inside one page that every row of it reaches into is one address and a lane's part of it
-  const bool one_page = !LIST && a.page_shift >= 5;
-  const int first_inside = (lo + 31) & ~31, last_inside = pos - 31;
-  const long lane_at = (lane / Geo::kCpr) * a.token_stride * kBytes + lane % Geo::kCpr * 16;
-  auto request = [&](int s, int page) {
-    const int s0 = __builtin_amdgcn_readfirstlane(s), page0 = __builtin_amdgcn_readfirstlane(page);
+  const unsigned char* __restrict__ kbase = (const unsigned char*)a.k + hk * a.head_stride * kBytes + lane % Geo::kCpr * 16;
+  const unsigned char* __restrict__ vbase = (const unsigned char*)a.v + hk * a.head_stride * kBytes + lane % Geo::kCpr * 16;
+  // loads of a tile: keys, then values (PAIR: the keys by the first wave, the values by the second)
+  auto is_value = [&](int i) { return PAIR ? second == 1 : i >= Geo::kNi; };
+  auto row_of = [&](int i) { return i % Geo::kNi * Geo::kRpi + lane / Geo::kCpr; };
+  uint4 x[Geo::kDepth][Geo::kLoads];
+  float scale[Geo::kDepth];
+  uint32_t valid[Geo::kDepth];                  // rows of the tile in registers that there are
+  // (A row that is none is read from the first row of the pool and cleared on its way into LDS: no load waits for a branch.)
+  auto request = [&](auto slot_number, int s, int page) {
+    constexpr int d = slot_number;
+    const bool ok = counts(s, page);
     const int o = s & ((1 << a.page_shift) - 1);
-    const bool ok = (uint32_t)page < (uint32_t)a.n_pages;
-    valid = (uint32_t)__builtin_amdgcn_ballot_w64(ok);
-    if (one_page && s0 >= first_inside && s0 <= last_inside && (uint32_t)page0 < (uint32_t)a.n_pages) {
-      const long at = (page0 * a.page_stride + (s0 & ((1 << a.page_shift) - 1)) * a.token_stride) * kBytes;
-      const unsigned char *ks = kbase + at, *vs = vbase + at;
-      const long step = Geo::kRpi * a.token_stride * kBytes;
+    valid[d] = (uint32_t)__builtin_amdgcn_ballot_w64(ok);
+    long at[Geo::kNi];
+    if (!LIST && a.page_shift >= 5 && valid[d] == 0xffffffffu) {
+      // the whole tile lies in one page: one address and a lane's part of it
+      const int o0 = __builtin_amdgcn_readfirstlane(o), page0 = __builtin_amdgcn_readfirstlane(page);
+      const long first = (page0 * a.page_stride + o0 * a.token_stride) * kBytes;
+      const long mine = lane / Geo::kCpr * a.token_stride * kBytes, step = Geo::kRpi * a.token_stride * kBytes;
 #pragma unroll
-      for (int i = 0; i < Geo::kNi; ++i) {
-        kr[i] = *reinterpret_cast<const uint4*>(ks + i * step + lane_at);
-        vr[i] = *reinterpret_cast<const uint4*>(vs + i * step + lane_at);
-      }
+      for (int i = 0; i < Geo::kNi; ++i) at[i] = first + i * step + mine;
     } else {
-      const long row = ok ? (page * a.page_stride + o * a.token_stride) * kBytes : -1;
+      const long row = ok ? (page * a.page_stride + o * a.token_stride) * kBytes : 0;
+      if (half == 0) row_at[col] = row;
+      wave_lds_order();
 #pragma unroll
-      for (int i = 0; i < Geo::kNi; ++i) {
-        const int r = i * Geo::kRpi + lane / Geo::kCpr;
-        const uint32_t lo = __shfl((uint32_t)row, r), hi = __shfl((uint32_t)((uint64_t)row >> 32), r);
-        const long at = (long)((uint64_t)hi << 32 | lo);
-        kr[i] = vr[i] = make_uint4(0, 0, 0, 0);
-        if (at >= 0) {
-          kr[i] = *reinterpret_cast<const uint4*>(kbase + at + lane % Geo::kCpr * 16);
-          vr[i] = *reinterpret_cast<const uint4*>(vbase + at + lane % Geo::kCpr * 16);
-        }
-      }
+      for (int i = 0; i < Geo::kNi; ++i) at[i] = row_at[row_of(i)];
+      wave_lds_order();
+    }
+#pragma unroll
+    for (int i = 0; i < Geo::kLoads; ++i)
+      x[d][i] = *reinterpret_cast<const uint4*>((is_value(i) ? vbase : kbase) + at[i % Geo::kNi]);
+    if constexpr (KDT == 2) {
+      const long slot = ok ? ((long)page << a.page_shift) + o : 0;
+      // lanes 0 .. 31 the keys' scales, 32 .. 63 the values' (PAIR: each wave its own, twice)
+      scale[d] = ((PAIR ? second : half) ? a.v_scale : a.k_scale)[slot * a.H_kv + hk];
+      scale[d] = ok ? scale[d] : 0.f;
+    }
+  };
+  auto deposit = [&](auto slot_number, unsigned char* kt, unsigned char* vt) {
+    constexpr int d = slot_number;
+    if (valid[d] != 0xffffffffu) {
+#pragma unroll
+      for (int i = 0; i < Geo::kLoads; ++i)
+        if (!(valid[d] >> row_of(i) & 1)) x[d][i] = make_uint4(0, 0, 0, 0);
+    }
+#pragma unroll
+    for (int i = 0; i < Geo::kLoads; ++i) {
+      if (is_value(i)) store_chunk<D, KDT, true>(vt, row_of(i), lane % Geo::kCpr, x[d][i]);
+      else store_chunk<D, KDT, false>(kt, row_of(i), lane % Geo::kCpr, x[d][i]);
     }
     if constexpr (KDT == 2) {
-      const long slot = ((long)page << a.page_shift) + o;
-      scale = ok ? (half ? a.v_scale : a.k_scale)[slot * a.H_kv + hk] : 0.f;
+      float* sc = reinterpret_cast<float*>(vt + Geo::kTile);                   // 32 key scales, 32 value scales
+      if (!PAIR) sc[lane] = scale[d];
+      else if (half == 0) sc[second * 32 + col] = scale[d];
     }
   };
 
-  const int read_key = RowTile<D>::read_key(), read_value = RowTile<D>::read_value();
-  int tile = begin + wave;
-  int s1 = position(tile), s2 = position(tile + kRowWaves);
-  request(s1, page_of(s1));
-  int p2 = page_of(s2);
-  int s3 = position(tile + 2 * kRowWaves);
-  for (; tile < end; tile += kRowWaves) {
-    const uint32_t keys = valid;
+  // page lookups run one tile ahead of the rows, list entries two
+  int tile = begin + lead, s_next, p_next, s_after;
+  RowState<D> st[1];
+  {
+    constexpr int kD = Geo::kDepth;
+    int s[kD + 2], p[kD + 1];
 #pragma unroll
-    for (int i = 0; i < Geo::kNi; ++i) {
-      const int r = i * Geo::kRpi + lane / Geo::kCpr;
-      store_chunk<D, KDT, false>(kt, r, lane % Geo::kCpr, kr[i]);
-      store_chunk<D, KDT, true>(vt, r, lane % Geo::kCpr, vr[i]);
-    }
-    if constexpr (KDT == 2) sc[lane] = scale;
-    wave_lds_order();
-    request(s2, p2);
-    s2 = s3;
-    p2 = page_of(s2);
-    s3 = position(tile + 3 * kRowWaves);
-
-    f32x16 s[NQ][1];
-    bf16x8 p[NQ][2];
-    score_tile<D, 1, NQ>(st, kt, renewed(read_key), s);
-    if constexpr (KDT == 2) {
+    for (int i = 0; i < kD + 2; ++i) s[i] = position(tile + i * kRowWaves);
 #pragma unroll
-      for (int q = 0; q < NQ; ++q) scale_scores<1>(s[q], sc);
-    }
-    if (keys != 0xffffffffu) {
-      asm volatile("");                    // (a branch, not selects for every tile)
-#pragma unroll
-      for (int q = 0; q < NQ; ++q) hide_keys(s[q][0], keys);
-    }
-#pragma unroll
-    for (int q = 0; q < NQ; ++q) softmax_tile<D, KDT, 1>(st[q], s[q], p[q], a.scale_log2, sc + 32);
-    add_values<D, 1, NQ>(st, vt, renewed(read_value), p);
-    wave_lds_order();
+    for (int i = 0; i < kD + 1; ++i) p[i] = page_of(s[i]);
+    steps([&](auto d) { request(d, s[d], p[d]); }, std::make_integer_sequence<int, kD>{});
+    s_next = s[kD];
+    p_next = p[kD];
+    s_after = s[kD + 1];
+    int r = r0 + col;                           // (columns beyond the last head repeat it and are not stored)
+    if (r >= a.G) r = a.G - 1;
+    st[0].clear();
+    st[0].load_q((const uint16_t*)a.q + ((long)t * a.H + hk * a.G + r) * D);
   }
-
-  // the waves' shares of every row, joined 32 rows at a time
-  float* part = reinterpret_cast<float*>(lds);             // [wave][D][32]
-#pragma unroll
-  for (int q = 0; q < NQ; ++q) {
-    const float l = add_halves(st[q].l);
-    __syncthreads();
-    if (half == 0) {
-      join[(wave * 32 + col) * 2] = st[q].m;
-      join[(wave * 32 + col) * 2 + 1] = l;
-    }
-    __syncthreads();
-    float top = neg_inf();
-#pragma unroll
-    for (int w = 0; w < kRowWaves; ++w) top = fmaxf(top, join[(w * 32 + col) * 2]);
-    const float base = top == neg_inf() ? 0.f : top;
-    float sum = 0.f;
-#pragma unroll
-    for (int w = 0; w < kRowWaves; ++w)
-      sum = __builtin_fmaf(__builtin_amdgcn_exp2f(join[(w * 32 + col) * 2] - base), join[(w * 32 + col) * 2 + 1], sum);
-    const float f = __builtin_amdgcn_exp2f(st[q].m - base);
-#pragma unroll
-    for (int dt = 0; dt < D / 32; ++dt)
-#pragma unroll
-      for (int i = 0; i < 16; ++i)
-        part[(wave * D + dt * 32 + 8 * (i >> 2) + 4 * half + (i & 3)) * 32 + col] = st[q].o[dt][i] * f;
-    __syncthreads();
-    const int r = r0 + q * 32 + col;
-    if (r < a.G) {
-      const long row = (long)t * a.H + hk * a.G + r;
-#pragma unroll
-      for (int j = 0; j < D / 32; ++j) {
-        const int e = ((threadIdx.x >> 5) * (D / 32) + j) * 4;
-        float x[4];
-#pragma unroll
-        for (int c = 0; c < 4; ++c) {
-          x[c] = 0.f;
-#pragma unroll
-          for (int w = 0; w < kRowWaves; ++w) x[c] += part[(w * D + e + c) * 32 + col];
-        }
-        const float4 o = make_float4(x[0], x[1], x[2], x[3]);
-        if (a.splits > 1) store_result<true>(a, split, row, D, e, o, top, sum);
-        else store_result<false>(a, split, row, D, e, o, top, sum);
+  const int read_key = RowTile<D>::read_key(), read_value = RowTile<D>::read_value();
+  int turn = 0;
+  auto iterate = [&](auto slot_number) {
+    constexpr int d = slot_number;
+    unsigned char* kt = ring + (PAIR ? turn * Geo::kStage : 0);
+    unsigned char* vt = kt + Geo::kTile;
+    const float* sc = reinterpret_cast<const float*>(vt + Geo::kTile);
+    const uint32_t keys = valid[d];
+    deposit(slot_number, kt, vt);
+    if constexpr (PAIR) lds_barrier();
+    else wave_lds_order();
+    request(slot_number, s_next, p_next);
+    s_next = s_after;
+    p_next = page_of(s_next);
+    s_after = position(tile + (Geo::kDepth + 2) * kRowWaves);
+    if (!PAIR || tile < end) {
+      f32x16 s[1][1];
+      bf16x8 p[1][2];
+      score_tile<D, 1, 1>(st, kt, renewed(read_key), s);
+      if constexpr (KDT == 2) scale_scores<1>(s[0], sc);
+      if (keys != 0xffffffffu) {
+        asm volatile("");                       // (a branch, not selects for every tile)
+        hide_keys(s[0][0], keys);
       }
+      softmax_tile<D, KDT, 1>(st[0], s[0], p[0], a.scale_log2, sc + 32);
+      add_values<D, 1, 1>(st, vt, renewed(read_value), p);
+    }
+    if constexpr (!PAIR) wave_lds_order();
+    tile += kRowWaves;
+    turn ^= 1;
+  };
+  // (with PAIR all waves go round together, whether they have a tile left or not)
+  auto more = [&]() { return PAIR ? tile - lead < end : tile < end; };
+  while (more())
+    steps(
+        [&](auto d) {
+          if (more()) iterate(d);
+        },
+        std::make_integer_sequence<int, Geo::kDepth>{});
+
+  // the waves' shares of every row, joined
+  float* part = reinterpret_cast<float*>(lds);                  // [wave][D][32]
+  const float l = add_halves(st[0].l);
+  if (half == 0) {
+    join[(wave * 32 + col) * 2] = st[0].m;
+    join[(wave * 32 + col) * 2 + 1] = l;
+  }
+  __syncthreads();
+  const int first = second * kRowWaves;                         // the waves with the same rows
+  float top = neg_inf();
+#pragma unroll
+  for (int w = 0; w < kRowWaves; ++w) top = fmaxf(top, join[((first + w) * 32 + col) * 2]);
+  const float base = top == neg_inf() ? 0.f : top;
+  float sum = 0.f;
+#pragma unroll
+  for (int w = 0; w < kRowWaves; ++w) {
+    const float* ml = join + ((first + w) * 32 + col) * 2;
+    sum = __builtin_fmaf(__builtin_amdgcn_exp2f(ml[0] - base), ml[1], sum);
+  }
+  const float f = __builtin_amdgcn_exp2f(st[0].m - base);
+#pragma unroll
+  for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+    for (int i = 0; i < 16; ++i)
+      part[(wave * D + dt * 32 + 8 * (i >> 2) + 4 * half + (i & 3)) * 32 + col] = st[0].o[dt][i] * f;
+  __syncthreads();
+  const int r = r0 + col;
+  if (r < a.G) {
+    const long row = (long)t * a.H + hk * a.G + r;
+#pragma unroll
+    for (int j = 0; j < D / 32; ++j) {
+      const int e = ((threadIdx.x >> 5 & 7) * (D / 32) + j) * 4;
+      float y[4];
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        y[c] = 0.f;
+#pragma unroll
+        for (int w = 0; w < kRowWaves; ++w) y[c] += part[((first + w) * D + e + c) * 32 + col];
+      }
+      const float4 o = make_float4(y[0], y[1], y[2], y[3]);
+      if (a.splits > 1) store_result<true>(a, split, row, D, e, o, top, sum);
+      else store_result<false>(a, split, row, D, e, o, top, sum);
     }
   }
 }
@@ -867,10 +910,10 @@ struct ChunkGeom {
 
 // 16 or 4 bytes per lane from `src` to LDS byte lds + 16 (or 4) * lane.
 __device__ __forceinline__ void dma16(uint32_t lds, const void* src) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds), "v"(src) : "memory", "m0");
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds), "v"(src) : "memory");
 }
 __device__ __forceinline__ void dma4(uint32_t lds, const void* src) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(lds), "v"(src) : "memory", "m0");
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(lds), "v"(src) : "memory");
 }
 template <int N>
 __device__ __forceinline__ void dma_left() {   // until at most N requests of this wave are under way
@@ -1124,11 +1167,13 @@ static __global__ __launch_bounds__(512, 2) void k_attn_chunk(AttnArgs a) {
     }
     Where at;
     constexpr int kProducts = D / 4;
+    __builtin_amdgcn_s_setprio(3);           // (the wave that multiplies goes first: 0.5 % at 1024 new tokens behind 64K)
     products<D>(st[0], lds + key_tile(r1), renewed(read_key), s[0], lds + value_tile(r), renewed(read_value), p[0], [&](int i) {
       if (i == 1) at = where(asked);
       // (fp8: the buffer of the step before the one that is widened now)
       if (i == kProducts / 4) request(asked, at, KDT == 2 ? (group == 0 ? r1 : r2) : asked & 3, tile + 7 + (KDT == 2));
     });
+    __builtin_amdgcn_s_setprio(0);
     if (dropped)
       add_odd_values<D, KDT>(st[0], (const unsigned char*)a.v + hk * a.head_stride * kBytes, offsets + (tile & 7) * kChunkKeys,
                              slots + (tile & 7) * kChunkKeys, a.v_scale + hk, a.H_kv, base);

@@ -57,7 +57,7 @@ int check_attention(const hisa_queries* q, const hisa_cache* c, int32_t k) {
 enum AttnKernel { ATTN_PLAIN, ATTN_ROWS, ATTN_CHUNK };
 struct AttnPlan {
   AttnKernel kernel;
-  int row_tiles;      // ATTN_ROWS: 32 heads each, per wave
+  bool pair;          // ATTN_ROWS: 64 heads per workgroup, not 32
   long units;         // tiles of query rows, of one KV head
   int splits;         // parts of their keys
   size_t ws_bytes;
@@ -75,10 +75,11 @@ AttnPlan plan_attention(const hisa_queries* q, const hisa_cache* c, int32_t k) {
     want = 1024;
   } else if (k || T <= c->n_seq) {
     p.kernel = ATTN_ROWS;
-    p.row_tiles = G > 32 ? 2 : 1;
-    p.units = T * ((G + 32 * p.row_tiles - 1) / (32 * p.row_tiles));
+    p.pair = G > 32;
+    const long heads = p.pair ? 64 : 32;
+    p.units = T * ((G + heads - 1) / heads);
     most = (keys + 255) / 256;
-    want = 2048;
+    want = k ? 512 : 2048;
   } else {
     p.kernel = ATTN_CHUNK;
     p.units = T * G / kChunkRows + c->n_seq;
@@ -123,19 +124,19 @@ AttnArgs attention_args(const hisa_queries* q, const hisa_cache* c, float scale,
   return a;
 }
 
-template <int D, int KDT, int NQ, bool LIST>
+template <int D, int KDT, bool PAIR, bool LIST>
 int launch_rows(const AttnArgs& a, dim3 grid, hipStream_t st) {
-  constexpr auto kern = k_attn_rows<D, KDT, NQ, LIST>;
-  constexpr int lds = RowGeom<D, KDT>::kLds;
-  if (lds > 65536 && raise_lds_limit<kern>(lds)) return HISA_ERR_LAUNCH;
-  hipLaunchKernelGGL(kern, grid, dim3(64 * kRowWaves), lds, st, a);
+  using Geo = RowGeom<D, KDT, PAIR>;
+  constexpr auto kern = k_attn_rows<D, KDT, PAIR, LIST>;
+  if (Geo::kLds > 65536 && raise_lds_limit<kern>(Geo::kLds)) return HISA_ERR_LAUNCH;
+  hipLaunchKernelGGL(kern, grid, dim3(64 * Geo::kWaves), Geo::kLds, st, a);
   return HISA_OK;
 }
 
 template <int D, int KDT, bool LIST>
 int launch_mfma(const AttnArgs& a, const AttnPlan& p, dim3 grid, hipStream_t st) {
   if (p.kernel == ATTN_ROWS)
-    return p.row_tiles == 2 ? launch_rows<D, KDT, 2, LIST>(a, grid, st) : launch_rows<D, KDT, 1, LIST>(a, grid, st);
+    return p.pair ? launch_rows<D, KDT, true, LIST>(a, grid, st) : launch_rows<D, KDT, false, LIST>(a, grid, st);
   if constexpr (!LIST) {
     constexpr auto kern = k_attn_chunk<D, KDT>;
     constexpr int lds = ChunkGeom<D, KDT>::kLds;
