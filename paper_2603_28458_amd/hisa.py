@@ -387,6 +387,20 @@ def _need(t, name: str, dtypes, shape=None, device=None, contiguous: bool = True
     return t
 
 
+def _fits(t, dtype, shape, dev: int) -> bool:
+    """What _need asks of a tensor, in one go: most calls pass, and a small call's time is its host side."""
+    return isinstance(t, torch.Tensor) and t.dtype is dtype and t.shape == shape and t.get_device() == dev and t.is_contiguous()
+
+
+def _gpu_of(t, name: str) -> int:
+    """Index of the GPU that a call's first tensor lives on."""
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name}: a tensor is needed, got {type(t).__name__}")
+    if not _on_gpu(t):
+        raise ValueError(f"{name}: not on the GPU ({t.device})")
+    return t.get_device()
+
+
 _I32 = (torch.int32,)
 _F32 = (torch.float32,)
 _STORED = {HISA_F32: (torch.float32,), HISA_BF16: (torch.bfloat16,),
@@ -396,8 +410,8 @@ _STORED = {HISA_F32: (torch.float32,), HISA_BF16: (torch.bfloat16,),
 class _on:
     """The GPU that the tensors live on as the current one while a call is enqueued (a no-op if it is already)."""
 
-    def __init__(self, device):
-        self.guard = torch.cuda.device(device) if device.index != torch.cuda.current_device() else None
+    def __init__(self, index: int):
+        self.guard = torch.cuda.device(index) if index != torch.cuda.current_device() else None
 
     def __enter__(self):
         if self.guard is not None:
@@ -407,6 +421,14 @@ class _on:
         if self.guard is not None:
             self.guard.__exit__(*exc)
         return False
+
+
+def _call(fn, dev: int, stream, *args) -> int:
+    """fn(*args, stream) with GPU `dev` current."""
+    if dev == torch.cuda.current_device():
+        return fn(*args, _stream(stream))
+    with _on(dev):
+        return fn(*args, _stream(stream))
 
 
 @dataclass
@@ -423,7 +445,17 @@ class Cache:
     k_scale: Optional[torch.Tensor] = None
     v_scale: Optional[torch.Tensor] = None
 
+    def __setattr__(self, name, value):
+        object.__setattr__(self, name, value)
+        self.__dict__.pop("_c", None)
+
+    def __getstate__(self):  # (copies build a struct of their own)
+        return {name: value for name, value in self.__dict__.items() if name not in ("_c", "_laid")}
+
     def __post_init__(self):
+        self.check()
+
+    def check(self):
         if self.dtype not in _STORED:
             raise ValueError(f"dtype: unknown code {self.dtype}")
         if self.k.dim() != 4:
@@ -448,12 +480,23 @@ class Cache:
             _need(self.seq_len, "seq_len", _I32, None if self.block_table is None else self.block_table.shape[:1], dev)
 
     def c(self) -> _Cache:
-        n, page, H_kv, d = self.k.shape
-        s = self.k.stride()
-        n_seq, max_pages = (0, 0) if self.block_table is None else self.block_table.shape
-        return _Cache(self.k.data_ptr(), None if self.v is None else self.v.data_ptr(), _ptr(self.k_scale),
-                      _ptr(self.v_scale), _ptr(self.block_table), _ptr(self.seq_len), s[0], s[1], s[2], n, page, n_seq,
-                      max_pages, H_kv, d, self.dtype)
+        k, v, ks, vs, table, length = self.k, self.v, self.k_scale, self.v_scale, self.block_table, self.seq_len
+        laid = (k.shape, k.stride(), None if table is None else table.shape)
+        c = self.__dict__.get("_c")
+        if c is None or self._laid != laid:
+            self.check()
+            n_seq, max_pages = laid[2] or (0, 0)
+            c = _Cache(None, None, None, None, None, None, *laid[1][:3], *laid[0][:2], n_seq, max_pages, *laid[0][2:],
+                       self.dtype)
+            self.__dict__.update(_laid=laid, _c=c)
+        # The sizes stay while the tensors keep theirs (the struct costs 3 us to build); where memory lies is asked anew.
+        c.k = k.data_ptr()
+        c.v = None if v is None else v.data_ptr()
+        c.k_scale = None if ks is None else ks.data_ptr()
+        c.v_scale = None if vs is None else vs.data_ptr()
+        c.block_table = None if table is None else table.data_ptr()
+        c.seq_len = None if length is None else length.data_ptr()
+        return c
 
 
 @dataclass
@@ -487,29 +530,31 @@ def hisa_page_tables(ctx_len: torch.Tensor, new_len: torch.Tensor, block_table: 
                      stream=None) -> PageTables:
     """Block tables (updated in place) and slot maps of a batch from its requests' lengths; s_max > 0: key_rows too, the
     tokens' rows in a padded key array [n_seq, s_max, d]."""
-    dev = ctx_len.device
-    _need(ctx_len, "ctx_len", _I32)
+    i32 = torch.int32
+    dev = _gpu_of(ctx_len, "ctx_len")
     n_seq = ctx_len.numel()
-    _need(ctx_len, "ctx_len", _I32, (n_seq,))
-    _need(new_len, "new_len", _I32, (n_seq,), dev)
-    _need(block_table, "block_table", _I32, None, dev)
-    _need(free_pages, "free_pages", _I32, (free_pages.numel(),), dev)
+    seqs, device = (n_seq,), ctx_len.device
+    _fits(ctx_len, i32, seqs, dev) or _need(ctx_len, "ctx_len", _I32, seqs)
+    _fits(new_len, i32, seqs, dev) or _need(new_len, "new_len", _I32, seqs, device)
+    n_free = free_pages.numel()
+    _fits(free_pages, i32, (n_free,), dev) or _need(free_pages, "free_pages", _I32, (n_free,), device)
     if block_table.dim() != 2 or block_table.shape[0] != n_seq:
         raise ValueError(f"block_table: shape {tuple(block_table.shape)}, needed is [{n_seq}, max_pages]")
+    _fits(block_table, i32, block_table.shape, dev) or _need(block_table, "block_table", _I32, None, device)
     if out is None:
-        out = PageTables.empty(n_seq, max(rows, 1), dev, key_rows=s_max > 0)
+        out = PageTables.empty(n_seq, max(rows, 1), device, key_rows=s_max > 0)
     else:
-        for name, t, n in (("seq_len", out.seq_len, n_seq), ("q_start", out.q_start, n_seq + 1),
-                           ("page_start", out.page_start, n_seq + 1), ("q_seq", out.q_seq, rows),
-                           ("q_pos", out.q_pos, rows), ("slots", out.slots, rows)):
-            _need(t, name, _I32, (n,), dev)
+        starts, row = (n_seq + 1,), (rows,)
+        for name, t, shape in (("seq_len", out.seq_len, seqs), ("q_start", out.q_start, starts),
+                               ("page_start", out.page_start, starts), ("q_seq", out.q_seq, row),
+                               ("q_pos", out.q_pos, row), ("slots", out.slots, row)):
+            _fits(t, i32, shape, dev) or _need(t, name, _I32, shape, device)
         if out.key_rows is not None:
-            _need(out.key_rows, "key_rows", _I32, (rows,), dev)
-    with _on(dev):
-        st = lib().hisa_page_tables(_ptr(ctx_len), _ptr(new_len), n_seq, _ptr(block_table), block_table.shape[1], page,
-                                    _ptr(free_pages), free_pages.numel(), rows, s_max, _ptr(out.seq_len),
-                                    _ptr(out.q_start), _ptr(out.page_start), _ptr(out.q_seq), _ptr(out.q_pos),
-                                    _ptr(out.slots), _ptr(out.key_rows), _stream(stream))
+            _fits(out.key_rows, i32, row, dev) or _need(out.key_rows, "key_rows", _I32, row, device)
+    st = _call(lib().hisa_page_tables, dev, stream, ctx_len.data_ptr(), new_len.data_ptr(), n_seq, block_table.data_ptr(),
+               block_table.shape[1], page, free_pages.data_ptr(), n_free, rows, s_max, out.seq_len.data_ptr(),
+               out.q_start.data_ptr(), out.page_start.data_ptr(), out.q_seq.data_ptr(), out.q_pos.data_ptr(),
+               out.slots.data_ptr(), None if out.key_rows is None else out.key_rows.data_ptr())
     _check(st, "hisa_page_tables")
     return out
 
@@ -518,26 +563,29 @@ def hisa_cache_append(cache: Cache, slots: torch.Tensor, k_new: torch.Tensor, v_
                       stream=None) -> None:
     """Rows k_new (and v_new) [T, H_kv, d] into the slots [T] of the cache, converted to its type.  The rows of a token
     are contiguous, tokens may lie further apart (a slice of a wider projection), keys and values alike."""
-    dev = cache.k.device
+    k = cache.k
+    dev = _gpu_of(k, "k")
     T = slots.numel()
-    _need(slots, "slots", _I32, (T,), dev)
-    H_kv, d = cache.k.shape[2:]
-    stride = k_new.stride(0) if k_new.dim() == 3 and T > 1 else H_kv * d
-    for name, t in (("k_new", k_new), ("v_new", v_new)):
-        if t is None:
-            continue
-        _need(t, name, (torch.float32, torch.bfloat16), (T, H_kv, d), dev, contiguous=False)
-        if t.dtype != k_new.dtype:
-            raise ValueError(f"v_new: {t.dtype}, k_new is {k_new.dtype}")
-        if T and not t[0].is_contiguous():
-            raise ValueError(f"{name}: the rows of a token are not contiguous")
-        if T > 1 and t.stride(0) != stride:
-            raise ValueError(f"v_new: tokens {t.stride(0)} elements apart, those of k_new {stride}")
-    cc = cache.c()
-    with _on(dev):
-        st = lib().hisa_cache_append(C.byref(cc), _ptr(slots), k_new.data_ptr(),
-                                     None if v_new is None else v_new.data_ptr(),
-                                     HISA_F32 if k_new.dtype == torch.float32 else HISA_BF16, stride, T, _stream(stream))
+    _fits(slots, torch.int32, (T,), dev) or _need(slots, "slots", _I32, (T,), k.device)
+    H_kv, d = k.shape[2:]
+    shape, dtype = (T, H_kv, d), k_new.dtype
+    stride = H_kv * d
+    if not (_fits(k_new, dtype, shape, dev) and (dtype is torch.bfloat16 or dtype is torch.float32)
+            and (v_new is None or _fits(v_new, dtype, shape, dev))):
+        # tokens further apart, or something that does not fit
+        stride = k_new.stride(0) if k_new.dim() == 3 and T > 1 else stride
+        for name, t in (("k_new", k_new), ("v_new", v_new)):
+            if t is None:
+                continue
+            _need(t, name, (torch.float32, torch.bfloat16), shape, k.device, contiguous=False)
+            if t.dtype != dtype:
+                raise ValueError(f"v_new: {t.dtype}, k_new is {dtype}")
+            if T and not t[0].is_contiguous():
+                raise ValueError(f"{name}: the rows of a token are not contiguous")
+            if T > 1 and t.stride(0) != stride:
+                raise ValueError(f"v_new: tokens {t.stride(0)} elements apart, those of k_new {stride}")
+    st = _call(lib().hisa_cache_append, dev, stream, cache.c(), slots.data_ptr(), k_new.data_ptr(),
+               None if v_new is None else v_new.data_ptr(), HISA_F32 if dtype is torch.float32 else HISA_BF16, stride, T)
     _check(st, "hisa_cache_append")
 
 
@@ -549,38 +597,40 @@ def hisa_attention_workspace_bytes(queries: Queries, cache: Cache, k: int = 0) -
 
 def _attention(name: str, queries: Queries, cache: Cache, index: torch.Tensor, k: int, scale, out, lse, want_lse, ws,
                stream):
-    q = queries.q
-    dev = cache.k.device
-    _need(q, "q", (torch.float32,) if queries.dtype == HISA_F32 else (torch.bfloat16,), None, dev)
-    if q.dim() != 3 or q.shape[2] != cache.k.shape[3]:
-        raise ValueError(f"q: shape {tuple(q.shape)}, needed is [T, H, {cache.k.shape[3]}]")
+    q, ck = queries.q, cache.k
+    dev, device = _gpu_of(ck, "k"), ck.device
+    dtype = torch.float32 if queries.dtype == HISA_F32 else torch.bfloat16
+    _fits(q, dtype, q.shape, dev) or _need(q, "q", (dtype,), None, device)
+    if q.dim() != 3 or q.shape[2] != ck.shape[3]:
+        raise ValueError(f"q: shape {tuple(q.shape)}, needed is [T, H, {ck.shape[3]}]")
     T, H, d = q.shape
+    rows, ptrs = (T,), []
     for what, t in (("q_seq", queries.q_seq), ("q_pos", queries.q_pos), ("q_lo", queries.q_lo)):
         if t is not None:
-            _need(t, what, _I32, (T,), dev)
+            _fits(t, torch.int32, rows, dev) or _need(t, what, _I32, rows, device)
+        ptrs.append(None if t is None else t.data_ptr())
     if out is None:
         out = torch.empty_like(q)
     else:
-        _need(out, "out", (q.dtype,), q.shape, dev)
+        _fits(out, dtype, q.shape, dev) or _need(out, "out", (dtype,), q.shape, device)
     if lse is not None:
-        _need(lse, "lse", _F32, (T, H), dev)
+        _fits(lse, torch.float32, (T, H), dev) or _need(lse, "lse", _F32, (T, H), device)
     elif want_lse:
-        lse = torch.empty((T, H), dtype=torch.float32, device=dev)
-    qc, cc = queries.c(), cache.c()
+        lse = torch.empty((T, H), dtype=torch.float32, device=device)
+    qc, cc = _Queries(q.data_ptr(), None, *ptrs, T, H, 0, queries.dtype), cache.c()
+    L = lib()
     if ws is None:
-        nbytes = int(lib().hisa_attention_workspace_bytes(C.byref(qc), C.byref(cc), k))
-        ws = torch.empty(nbytes, dtype=torch.uint8, device=dev) if nbytes else None
+        size = int(L.hisa_attention_workspace_bytes(qc, cc, k))
+        ws = torch.empty(size, dtype=torch.uint8, device=device) if size else None
     else:
-        _need(ws, "ws", (torch.uint8,), None, dev)
+        size = ws.numel()
+        _fits(ws, torch.uint8, ws.shape, dev) or _need(ws, "ws", (torch.uint8,), None, device)
     scale = d ** -0.5 if scale is None else float(scale)
-    size = 0 if ws is None else ws.numel()
-    with _on(dev):
-        if k:
-            st = lib().hisa_sparse_attention(C.byref(qc), C.byref(cc), _ptr(index), k, scale, _ptr(out), _ptr(lse),
-                                             _ptr(ws), size, _stream(stream))
-        else:
-            st = lib().hisa_paged_attention(C.byref(qc), C.byref(cc), _ptr(index), scale, _ptr(out), _ptr(lse), _ptr(ws),
-                                            size, _stream(stream))
+    ptrs = (scale, out.data_ptr(), None if lse is None else lse.data_ptr(), None if ws is None else ws.data_ptr(), size)
+    if k:
+        st = _call(L.hisa_sparse_attention, dev, stream, qc, cc, index.data_ptr(), k, *ptrs)
+    else:
+        st = _call(L.hisa_paged_attention, dev, stream, qc, cc, index.data_ptr(), *ptrs)
     _check(st, name)
     return out, lse
 
@@ -592,7 +642,8 @@ def hisa_paged_attention(queries: Queries, cache: Cache, q_start: torch.Tensor, 
     or None)."""
     if cache.block_table is None or cache.seq_len is None or cache.v is None:
         raise ValueError("cache: values, block_table and seq_len are needed")
-    _need(q_start, "q_start", _I32, (cache.block_table.shape[0] + 1,), cache.k.device)
+    shape = (cache.block_table.shape[0] + 1,)
+    _fits(q_start, torch.int32, shape, cache.k.get_device()) or _need(q_start, "q_start", _I32, shape, cache.k.device)
     return _attention("hisa_paged_attention", queries, cache, q_start, 0, scale, out, lse, want_lse, ws, stream)
 
 
@@ -603,7 +654,8 @@ def hisa_sparse_attention(queries: Queries, cache: Cache, topk_idx: torch.Tensor
     skipped).  Returns (out [T, H, d], lse [T, H] or None)."""
     if cache.block_table is None or cache.seq_len is None or cache.v is None:
         raise ValueError("cache: values, block_table and seq_len are needed")
-    _need(topk_idx, "topk_idx", _I32, None, cache.k.device)
+    _fits(topk_idx, torch.int32, topk_idx.shape, cache.k.get_device()) or _need(topk_idx, "topk_idx", _I32, None,
+                                                                                 cache.k.device)
     if topk_idx.dim() != 2 or topk_idx.shape[0] != queries.T or topk_idx.shape[1] < 1:
         raise ValueError(f"topk_idx: shape {tuple(topk_idx.shape)}, needed is [{queries.T}, k]")
     return _attention("hisa_sparse_attention", queries, cache, topk_idx, topk_idx.shape[1], scale, out, lse, want_lse, ws,

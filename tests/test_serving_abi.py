@@ -1,5 +1,6 @@
 """The calls around the indexer without a GPU: what they refuse, before anything is launched.  (Pointers are fake
 non-null values: a call that got past its checks here would fail the test by its status.)"""
+import copy
 import ctypes as C
 
 import pytest
@@ -205,14 +206,11 @@ def test_the_binding_refuses_types_shapes_and_strides(lib, monkeypatch):  # noqa
 
 
 def test_another_gpu_than_the_current_one_is_made_current_for_the_call(monkeypatch):
-    class Device:
-        index = 1
-
     seen = []
 
     class Guard:
-        def __init__(self, device):
-            seen.append(device.index)
+        def __init__(self, index):
+            seen.append(index)
 
         def __enter__(self):
             seen.append("in")
@@ -222,13 +220,37 @@ def test_another_gpu_than_the_current_one_is_made_current_for_the_call(monkeypat
 
     monkeypatch.setattr(hisa.torch.cuda, "current_device", lambda: 0)
     monkeypatch.setattr(hisa.torch.cuda, "device", Guard)
-    with hisa._on(Device()):
-        assert seen == [1, "in"]
-    assert seen == [1, "in", "out"]
-    Device.index = 0
-    with hisa._on(Device()):
-        pass
-    assert len(seen) == 3
+    monkeypatch.setattr(hisa, "_stream", lambda stream: seen.append("stream") or 5)
+    assert hisa._call(lambda *a: a, 1, None, 7, 8) == (7, 8, 5)
+    assert seen == [1, "in", "stream", "out"]
+    del seen[:]
+    assert hisa._call(lambda *a: a, 0, None, 7) == (7, 5)
+    assert seen == ["stream"]
+
+
+def test_a_cache_is_checked_again_after_a_change(monkeypatch):
+    monkeypatch.setattr(hisa, "_on_gpu", lambda t: True)
+    k = torch.zeros((4, 16, 2, 128), dtype=torch.bfloat16)
+    cache = hisa.Cache(k=k, v=k.clone(), dtype=hisa.HISA_BF16, block_table=torch.zeros((3, 2), dtype=torch.int32),
+                       seq_len=torch.zeros(3, dtype=torch.int32))
+    c = cache.c()
+    assert (c.n_pages, c.page, c.H_kv, c.d, c.n_seq, c.max_pages) == (4, 16, 2, 128, 3, 2)
+    cache.block_table = torch.zeros((3, 5), dtype=torch.int32)
+    assert cache.c().max_pages == 5 and cache.c().block_table == cache.block_table.data_ptr()
+    cache.block_table = torch.zeros((2, 5), dtype=torch.int32)
+    with pytest.raises(ValueError, match="seq_len"):
+        cache.c()
+    cache.seq_len = torch.zeros(2, dtype=torch.int32)
+    assert cache.c().n_seq == 2
+    other = copy.deepcopy(cache)
+    assert other.c().k == other.k.data_ptr() != cache.c().k
+    assert copy.copy(cache).c() is not cache.c()
+    cache.k.resize_(8, 8, 2, 128)
+    with pytest.raises(ValueError, match="v: shape"):
+        cache.c()
+    cache.v = cache.v.float()
+    with pytest.raises(ValueError, match="v: "):
+        cache.c()
 
 
 # ---- the oracle against a few numbers worked out by hand
