@@ -511,6 +511,25 @@ class PageTables:
     slots: torch.Tensor
     key_rows: Optional[torch.Tensor] = None
 
+    def __setattr__(self, name, value):
+        object.__setattr__(self, name, value)
+        self.__dict__.pop("_checked", None)
+
+    def pointers(self, n_seq: int, rows: int, dev: int, device) -> list:
+        """Where the seven tensors lie.  Their types and layout are checked once for a batch's sizes, and again if a
+        tensor is replaced or resized."""
+        tensors = (self.seq_len, self.q_start, self.page_start, self.q_seq, self.q_pos, self.slots, self.key_rows)
+        sizes = (n_seq, n_seq + 1, n_seq + 1, rows, rows, rows, rows)
+        if (self.__dict__.get("_checked") != (n_seq, rows, dev)
+                or any([t is not None and t.numel() != n for t, n in zip(tensors, sizes)])):
+            names = ("seq_len", "q_start", "page_start", "q_seq", "q_pos", "slots")
+            for name, t, n in zip(names, tensors, sizes):
+                _need(t, name, _I32, (n,), device)
+            if self.key_rows is not None:
+                _need(self.key_rows, "key_rows", _I32, (rows,), device)
+            self.__dict__["_checked"] = (n_seq, rows, dev)
+        return [None if t is None else t.data_ptr() for t in tensors]
+
     @property
     def pages_used(self) -> torch.Tensor:
         """[1]: how many of the free pages are in use now (more than there were: too few)."""
@@ -542,19 +561,10 @@ def hisa_page_tables(ctx_len: torch.Tensor, new_len: torch.Tensor, block_table: 
         raise ValueError(f"block_table: shape {tuple(block_table.shape)}, needed is [{n_seq}, max_pages]")
     _fits(block_table, i32, block_table.shape, dev) or _need(block_table, "block_table", _I32, None, device)
     if out is None:
-        out = PageTables.empty(n_seq, max(rows, 1), device, key_rows=s_max > 0)
-    else:
-        starts, row = (n_seq + 1,), (rows,)
-        for name, t, shape in (("seq_len", out.seq_len, seqs), ("q_start", out.q_start, starts),
-                               ("page_start", out.page_start, starts), ("q_seq", out.q_seq, row),
-                               ("q_pos", out.q_pos, row), ("slots", out.slots, row)):
-            _fits(t, i32, shape, dev) or _need(t, name, _I32, shape, device)
-        if out.key_rows is not None:
-            _fits(out.key_rows, i32, row, dev) or _need(out.key_rows, "key_rows", _I32, row, device)
+        out = PageTables.empty(n_seq, rows, device, key_rows=s_max > 0)
     st = _call(lib().hisa_page_tables, dev, stream, ctx_len.data_ptr(), new_len.data_ptr(), n_seq, block_table.data_ptr(),
-               block_table.shape[1], page, free_pages.data_ptr(), n_free, rows, s_max, out.seq_len.data_ptr(),
-               out.q_start.data_ptr(), out.page_start.data_ptr(), out.q_seq.data_ptr(), out.q_pos.data_ptr(),
-               out.slots.data_ptr(), None if out.key_rows is None else out.key_rows.data_ptr())
+               block_table.shape[1], page, free_pages.data_ptr(), n_free, rows, s_max,
+               *out.pointers(n_seq, rows, dev, device))
     _check(st, "hisa_page_tables")
     return out
 
