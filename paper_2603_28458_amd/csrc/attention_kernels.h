@@ -75,169 +75,6 @@ __device__ __forceinline__ void store_four(const AttnArgs& a, long row, int e, f
   }
 }
 
-// fp32 queries and rows: one query token, up to 8 heads of one KV head, one part of its keys per workgroup of 4 waves.  A
-// wave takes every fourth tile of 64 keys: a key per lane for the scores, then 4 output columns per lane for the values.
-constexpr int kPlainHeads = 8, kPlainMaxD = 256;
-
-template <bool LIST>
-static __global__ __launch_bounds__(256) void k_attn_plain(AttnArgs a) {
-  __shared__ float qs[kPlainHeads][kPlainMaxD];
-  __shared__ float ps[4][kPlainHeads][64];
-  __shared__ long vrow[4][64];
-  __shared__ float join_o[4][kPlainHeads][kPlainMaxD];
-  __shared__ float join_ml[4][kPlainHeads][2];
-  const int lane = lane_id(), wave = threadIdx.x >> 6;
-  const int chunks = (a.G + kPlainHeads - 1) / kPlainHeads;
-  long id = blockIdx.x;
-  const int split = (int)(id % a.splits);
-  id /= a.splits;
-  const int chunk = (int)(id % chunks);
-  id /= chunks;
-  const int hk = (int)(id % a.H_kv), t = (int)(id / a.H_kv);
-  const int h0 = hk * a.G + chunk * kPlainHeads;
-  const int heads = a.G - chunk * kPlainHeads < kPlainHeads ? a.G - chunk * kPlainHeads : kPlainHeads;
-
-  int n, begin = 0, end;
-  if constexpr (LIST) {
-    n = a.q_seq ? a.q_seq[t] : 0;
-    end = (uint32_t)n < (uint32_t)a.n_seq ? a.n_list : 0;
-    if (end == 0) n = 0;
-  } else {
-    n = last_seq(a.n_seq, [&](int i) { return a.q_start[i] <= t; });
-    if (t < a.q_start[n] || t >= a.q_start[n + 1]) return;       // nobody's row
-    const int len = clamp_len(a, n);
-    const int pos = a.q_pos ? a.q_pos[t] : a.seq_len[n] - a.q_start[n + 1] + t;
-    end = pos < len ? pos + 1 : len;
-    if (a.q_lo && a.q_lo[t] > 0) begin = a.q_lo[t];
-  }
-  const int len = clamp_len(a, n);
-  const int32_t* __restrict__ row = a.table + (long)n * a.max_pages;
-  if (a.splits > 1 && end > begin) {                              // this part: whole tiles of 64
-    const long tiles = (end - (long)begin + 63) / 64;
-    const int b0 = begin;
-    begin = b0 + (int)(tiles * split / a.splits) * 64;
-    const long stop = b0 + (tiles * (split + 1) / a.splits) * 64;
-    end = stop < end ? (int)stop : end;
-  }
-
-  for (int i = threadIdx.x; i < heads * (a.d / 4); i += 256) {
-    const int g = i / (a.d / 4), e = i % (a.d / 4) * 4;
-    const float4 x = load_f32x4(a.q, ((long)t * a.H + h0 + g) * a.d + e);
-    qs[g][e] = x.x * a.scale_log2;
-    qs[g][e + 1] = x.y * a.scale_log2;
-    qs[g][e + 2] = x.z * a.scale_log2;
-    qs[g][e + 3] = x.w * a.scale_log2;
-  }
-  __syncthreads();
-
-  float m[kPlainHeads], l[kPlainHeads];
-  float4 o[kPlainHeads];
-#pragma unroll
-  for (int g = 0; g < kPlainHeads; ++g) {
-    m[g] = neg_inf();
-    l[g] = 0.f;
-    o[g] = make_float4(0.f, 0.f, 0.f, 0.f);
-  }
-  const bool mine = lane * 4 < a.d;
-  for (long tile = (long)begin + wave * 64; tile < end; tile += 256) {
-    const int c = (int)tile + lane;
-    long at = -1;                         // this lane's row, if the query sees it
-    if (c < end) {
-      const int s = LIST ? a.list[(long)t * a.n_list + c] : c;
-      const int page = s >= 0 && s < len ? row[s >> a.page_shift] : -1;
-      if ((uint32_t)page < (uint32_t)a.n_pages)
-        at = page * a.page_stride + (s & ((1 << a.page_shift) - 1)) * a.token_stride + hk * a.head_stride;
-    }
-    float x[kPlainHeads];
-#pragma unroll
-    for (int g = 0; g < kPlainHeads; ++g) x[g] = 0.f;
-    if (at >= 0) {
-      for (int e = 0; e < a.d; e += 4) {
-        const float4 kk = load_f32x4(a.k, at + e);
-#pragma unroll
-        for (int g = 0; g < kPlainHeads; ++g)
-          x[g] = __builtin_fmaf(qs[g][e], kk.x,
-                 __builtin_fmaf(qs[g][e + 1], kk.y, __builtin_fmaf(qs[g][e + 2], kk.z, __builtin_fmaf(qs[g][e + 3], kk.w, x[g]))));
-      }
-    }
-    vrow[wave][lane] = at;
-#pragma unroll
-    for (int g = 0; g < kPlainHeads; ++g) {
-      if (at < 0) x[g] = neg_inf();
-      float top = x[g];
-      for (int s = 1; s < 64; s <<= 1) top = fmaxf(top, __shfl_xor(top, s));
-      const float mn = fmaxf(m[g], top);
-      const float base = mn == neg_inf() ? 0.f : mn;
-      const float p = at < 0 ? 0.f : __builtin_amdgcn_exp2f(x[g] - base);
-      const float shrink = __builtin_amdgcn_exp2f(m[g] - base);
-      float sum = p;
-      for (int s = 1; s < 64; s <<= 1) sum += __shfl_xor(sum, s);
-      l[g] = l[g] * shrink + sum;
-      o[g].x *= shrink;
-      o[g].y *= shrink;
-      o[g].z *= shrink;
-      o[g].w *= shrink;
-      m[g] = mn;
-      ps[wave][g][lane] = p;
-    }
-    wave_lds_order();
-    for (int j = 0; j < 64; ++j) {
-      const long vat = vrow[wave][j];
-      if (vat < 0 || !mine) continue;
-      const float4 vv = load_f32x4(a.v, vat + lane * 4);
-#pragma unroll
-      for (int g = 0; g < kPlainHeads; ++g) {
-        const float p = ps[wave][g][j];
-        o[g].x = __builtin_fmaf(p, vv.x, o[g].x);
-        o[g].y = __builtin_fmaf(p, vv.y, o[g].y);
-        o[g].z = __builtin_fmaf(p, vv.z, o[g].z);
-        o[g].w = __builtin_fmaf(p, vv.w, o[g].w);
-      }
-    }
-    wave_lds_order();
-  }
-#pragma unroll
-  for (int g = 0; g < kPlainHeads; ++g) {
-    if (mine) *reinterpret_cast<float4*>(&join_o[wave][g][lane * 4]) = o[g];
-    if (lane == 0) {
-      join_ml[wave][g][0] = m[g];
-      join_ml[wave][g][1] = l[g];
-    }
-  }
-  __syncthreads();
-  for (int i = threadIdx.x; i < heads * (a.d / 4); i += 256) {
-    const int g = i / (a.d / 4), e = i % (a.d / 4) * 4;
-    float top = neg_inf();
-    for (int w = 0; w < 4; ++w) top = fmaxf(top, join_ml[w][g][0]);
-    const float base = top == neg_inf() ? 0.f : top;
-    float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
-    float sum = 0.f;
-    for (int w = 0; w < 4; ++w) {
-      const float f = __builtin_amdgcn_exp2f(join_ml[w][g][0] - base);
-      sum += f * join_ml[w][g][1];
-      const float4 x = *reinterpret_cast<const float4*>(&join_o[w][g][e]);
-      s.x = __builtin_fmaf(f, x.x, s.x);
-      s.y = __builtin_fmaf(f, x.y, s.y);
-      s.z = __builtin_fmaf(f, x.z, s.z);
-      s.w = __builtin_fmaf(f, x.w, s.w);
-    }
-    const long r = (long)t * a.H + h0 + g;
-    if (a.splits > 1) {
-      const long pr = (long)split * a.T * a.H + r;
-      *reinterpret_cast<float4*>(a.part + pr * a.d + e) = s;
-      if (e == 0) {
-        float* ml = a.part + (long)a.splits * a.T * a.H * a.d + pr * 2;
-        ml[0] = top;
-        ml[1] = sum;
-      }
-    } else {
-      const float inv = sum == 0.f ? 0.f : 1.f / sum;
-      store_four<0>(a, r, e, make_float4(s.x * inv, s.y * inv, s.z * inv, s.w * inv));
-      if (e == 0 && a.lse) a.lse[r] = sum == 0.f ? neg_inf() : (base + log2f(sum)) * 0.693147180559945309f;
-    }
-  }
-}
-
 // ------------------------------------------------------------------------------------------
 // Matrix-core path (bf16 queries, bf16 or fp8 rows, d = 64 or 128).  Everything is computed transposed, keys (then
 // columns of the output) along the rows of the 32x32x16 MFMA and query rows along its columns: S^T = K Q^T, O^T = V^T P^T.
@@ -611,7 +448,7 @@ __device__ __forceinline__ void take_part(int& begin, int& end, int split, int s
 }
 
 // One result row: 4 columns at e of (t, h) row r, sums with maximum m and weight sum l.
-template <bool PART>
+template <int QDT, bool PART>
 __device__ __forceinline__ void store_result(const AttnArgs& a, int split, long r, int D, int e, float4 o, float m, float l) {
   if constexpr (PART) {
     const long pr = (long)split * a.T * a.H + r;
@@ -623,8 +460,280 @@ __device__ __forceinline__ void store_result(const AttnArgs& a, int split, long 
     }
   } else {
     const float inv = l == 0.f ? 0.f : 1.f / l;
-    store_four<1>(a, r, e, make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv));
+    store_four<QDT>(a, r, e, make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv));
     if (e == 0 && a.lse) a.lse[r] = l == 0.f ? neg_inf() : (m + log2f(l)) * 0.693147180559945309f;
+  }
+}
+
+// ---- fp32 queries and rows ---------------------------------------------------------------------
+// The same transposed products on the 32x32x2 fp32 MFMA (exact products, fp32 sums).  A workgroup takes 32 query rows of
+// one KV head (tokens of one sequence times heads; lists: heads of one token) and a part of their keys; each of 4 waves
+// works alone on every fourth tile of 32 keys, and the waves' results are joined at the end.  Operands come straight from
+// memory: of a key row lane half h reads elements 8 kk + 4 h + 0..3 and spends them on four products (a contraction may
+// take its index in any order), a value row is read 32 columns at a time by 32 lanes.  As the keys of a tile are used up the
+// values take their registers, and the next keys theirs: each is under way for as long as the other is multiplied.  The scores' accumulator holds keys
+// 8 j + 4 half + x in register 4 j + x, so product 4 j + x of the values takes those two keys and that register as it is.
+// Bound by memory where a KV head's group is small (8 D bytes per key), by the fp32 matrix units where 32 rows are real.
+constexpr int kF32MaxD = 256;
+
+template <int D>
+struct F32Geom {
+  static constexpr int kQ = D * 128;                          // [D / 8][64] of 16 bytes
+  static constexpr int kLoop = kQ + 4 * 256, kJoin = D * 512; // and row offsets [4][32]; or [4][D][32] to join
+  static constexpr int kMl = kLoop > kJoin ? kLoop : kJoin, kLds = kMl + 4 * 256;
+};
+
+template <int D, bool LIST>
+static __global__ __launch_bounds__(256, D > 128 ? 1 : 2) void k_attn_f32(AttnArgs a) {
+  using Geo = F32Geom<D>;
+  constexpr int kSteps = D / 8, kCols = D / 32;
+  constexpr int kKeep = kSteps < 16 ? kSteps : 16, kRows = D > 128 ? 8 : 16;   // key steps, value rows in registers
+  constexpr bool kPart = D == kF32MaxD;                       // rows may be shorter than D
+  extern __shared__ __align__(16) unsigned char lds[];
+  const int lane = lane_id(), half = lane >> 5, col = lane & 31;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  float4* qs = reinterpret_cast<float4*>(lds);
+  long* row_at = reinterpret_cast<long*>(lds + Geo::kQ) + wave * 32;
+  float* join = reinterpret_cast<float*>(lds + Geo::kMl);     // [wave][32][2]
+
+  uint32_t id = blockIdx.x;
+  const int hk = (int)(id % (uint32_t)a.H_kv);
+  id /= (uint32_t)a.H_kv;
+  const int split = (int)(id % (uint32_t)a.splits), unit = (int)(id / (uint32_t)a.splits);
+  int n, len, r0, rows, t_begin, begin, end;                  // tiles of 32 keys (list entries)
+  int t_end = 0;
+  if constexpr (LIST) {
+    const int head_tiles = (a.G + 31) / 32;
+    t_begin = unit / head_tiles;
+    r0 = (unit - t_begin * head_tiles) * 32;
+    rows = a.G;
+    n = a.q_seq ? a.q_seq[t_begin] : 0;
+    const bool none = (uint32_t)n >= (uint32_t)a.n_seq;
+    n = none ? 0 : n;
+    len = none ? 0 : clamp_len(a, n);
+    begin = 0;
+    end = (a.n_list + 31) / 32;
+  } else {
+    const RowUnit u = find_unit<32>(a, unit);
+    n = u.n;
+    t_begin = u.t_begin;
+    t_end = u.t_end;
+    r0 = u.r0;
+    rows = (t_end - t_begin) * a.G;
+    if (r0 < 0 || r0 >= rows || t_begin < 0 || t_end > a.T) return;
+    len = clamp_len(a, n);
+  }
+  int qr = r0 + col;
+  const bool mine = qr < rows;
+  if (!mine) qr = rows - 1;                                   // (columns beyond the last row repeat it and are not stored)
+  const int t = t_begin + qr / a.G;
+  const long row = (long)t * a.H + hk * a.G + qr % a.G;
+  Seen seen{0, 0x7fffffff};
+  int pos_min = 0x7fffffff, lo_max = 0, pos_max = 0x7fffffff, lo_min = 0;
+  if constexpr (!LIST) {
+    seen = seen_by(a, n, len, t, t_end);
+    pos_min = wave_min_int(seen.pos);
+    pos_max = wave_max_int(seen.pos);
+    lo_min = wave_min_int(seen.lo);
+    lo_max = wave_max_int(seen.lo);
+    begin = lo_min >> 5;
+    end = (pos_max + 32) >> 5;
+    if (pos_max < 0 || end < begin) end = begin;
+  }
+  if (a.splits > 1) take_part(begin, end, split, a.splits, 4);   // of at least one tile per wave
+
+  for (int kk = wave; kk < kSteps; kk += 4) {
+    const int e = kk * 8 + half * 4;
+    qs[kk * 64 + lane] = !kPart || e < a.d ? load_f32x4(a.q, row * a.d + e) : make_float4(0.f, 0.f, 0.f, 0.f);
+  }
+
+  const int32_t* __restrict__ table = a.table + (long)n * a.max_pages;
+  const int cap_last = (int)(((long)a.max_pages << a.page_shift) - 1);
+  auto position = [&](int tile) {            // of key `col` of a tile (or one that is no position)
+    if (tile >= end) return -1;
+    const int c = tile * 32 + col;
+    if constexpr (LIST) return c < a.n_list ? a.list[(long)t * a.n_list + c] : -1;
+    else return c;
+  };
+  auto page_of = [&](int s) {
+    const int in = s < 0 ? 0 : s > cap_last ? cap_last : s;
+    return table[in >> a.page_shift];
+  };
+  uint32_t valid;                            // keys of the tile that there are
+  long at;                                   // of key `col` (a row that is none: the pool's first, read and cleared)
+  auto locate = [&](int s, int page) {
+    const bool ok = (LIST ? s >= 0 && s < len : s >= lo_min && s <= pos_max) && (uint32_t)page < (uint32_t)a.n_pages;
+    valid = (uint32_t)__builtin_amdgcn_ballot_w64(ok);
+    at = ok ? page * a.page_stride + (s & ((1 << a.page_shift) - 1)) * a.token_stride : 0;
+  };
+  const float* __restrict__ kbase = (const float*)a.k + hk * a.head_stride + half * 4;
+  const float* __restrict__ vbase = (const float*)a.v + hk * a.head_stride;
+  float4 kx[kKeep];
+  float vx[kRows][kCols];
+  auto request_key = [&](int kk) {
+    kx[kk % kKeep] = load_f32x4(kbase, at + (kPart && kk * 8 + half * 4 >= a.d ? -half * 4 : kk * 8));   // (beyond a row: not used)
+  };
+  auto key_of = [&](int i) { return 8 * (i >> 2) + 4 * half + (i & 3); };   // of register i
+  auto request_value = [&](int i) {
+    const float* v = vbase + row_at[key_of(i)];
+#pragma unroll
+    for (int dt = 0; dt < kCols; ++dt) vx[i % kRows][dt] = v[kPart && dt * 32 + col >= a.d ? 0 : dt * 32 + col];
+  };
+  auto leave_rows = [&]() {                  // for request_value
+    wave_lds_order();
+    if (half == 0) row_at[col] = at;
+    wave_lds_order();
+  };
+
+  int tile = begin + wave;
+  int s_next = position(tile + 4), s_after = position(tile + 8);
+  {
+    const int s = position(tile), page = page_of(s);
+    locate(s, page);
+  }
+  int p_next = page_of(s_next);
+#pragma unroll
+  for (int kk = 0; kk < kKeep; ++kk) request_key(kk);
+  leave_rows();
+  float m = neg_inf(), l = 0.f;
+  f32x16 o[kCols];
+#pragma unroll
+  for (int dt = 0; dt < kCols; ++dt)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) o[dt][i] = 0.f;
+  __syncthreads();                           // (the queries)
+  for (; tile < end; tile += 4) {
+    const int base = tile * 32;
+    const uint32_t keys = valid;
+    const bool mixed = !LIST && (base + 31 > pos_min || base < lo_max);
+    f32x16 s;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) s[i] = 0.f;
+#pragma unroll
+    for (int kk = 0; kk < kSteps; ++kk) {
+      const float4 q = qs[kk * 64 + lane];
+      float4 k = kx[kk % kKeep];
+      if (kPart && kk * 8 + half * 4 >= a.d) k = make_float4(0.f, 0.f, 0.f, 0.f);
+      s = __builtin_amdgcn_mfma_f32_32x32x2f32(k.x, q.x, s, 0, 0, 0);
+      s = __builtin_amdgcn_mfma_f32_32x32x2f32(k.y, q.y, s, 0, 0, 0);
+      s = __builtin_amdgcn_mfma_f32_32x32x2f32(k.z, q.z, s, 0, 0, 0);
+      s = __builtin_amdgcn_mfma_f32_32x32x2f32(k.w, q.w, s, 0, 0, 0);
+      if (kk + kKeep < kSteps) request_key(kk + kKeep);
+      const int f = kk + kKeep - kSteps;
+#pragma unroll
+      for (int i = f < 0 ? 0 : f * kRows / kKeep; i < (f + 1) * kRows / kKeep; ++i) request_value(i);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    locate(s_next, p_next);
+    s_next = s_after;
+    p_next = page_of(s_next);
+    s_after = position(tile + 12);
+
+    float top = neg_inf();
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const int key = key_of(i);
+      const bool in = (keys >> key & 1u) && (LIST || (base + key >= seen.lo && base + key <= seen.pos));
+      s[i] = in ? s[i] * a.scale_log2 : neg_inf();
+      top = __builtin_elementwise_maximum(top, s[i]);
+    }
+    top = max_halves(top);
+    if (__builtin_amdgcn_ballot_w64(top > m + kSlack)) {
+      const float mn = fmaxf(m, top);
+      const float f = __builtin_amdgcn_exp2f(m - (mn == neg_inf() ? 0.f : mn));
+      m = mn;
+      l *= f;
+#pragma unroll
+      for (int dt = 0; dt < kCols; ++dt)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[dt][i] *= f;
+    }
+    const float off = m == neg_inf() ? 0.f : m;
+    float sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      s[i] = __builtin_amdgcn_exp2f(s[i] - off);
+      sum += s[i];
+    }
+    l += sum;
+
+    const bool clean = keys != 0xffffffffu || mixed;
+    bool odd = false;                        // (as in the tiles of bf16: what some rows must not meet is added apart)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      float (&v)[kCols] = vx[i % kRows];
+      if (clean) {
+        const bool there = keys >> key_of(i) & 1u;
+#pragma unroll
+        for (int dt = 0; dt < kCols; ++dt) {
+          const bool bad = mixed && !(__builtin_fabsf(v[dt]) < __builtin_inff());
+          odd |= there && bad;
+          if (!there || bad) v[dt] = 0.f;
+        }
+      }
+#pragma unroll
+      for (int dt = 0; dt < kCols; ++dt) o[dt] = __builtin_amdgcn_mfma_f32_32x32x2f32(v[dt], s[i], o[dt], 0, 0, 0);
+      if (i + kRows < 16) request_value(i + kRows);
+      const int f = i + kRows - 16;
+#pragma unroll
+      for (int kk = f < 0 ? 0 : f * kKeep / kRows; kk < (f + 1) * kKeep / kRows; ++kk) request_key(kk);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    if (__builtin_amdgcn_ballot_w64(odd)) {
+      for (int key = 0; key < 32; ++key) {
+        const bool in = (keys >> key & 1u) && base + key >= seen.lo && base + key <= seen.pos;
+        const float* v = vbase + row_at[key];
+#pragma unroll
+        for (int dt = 0; dt < kCols; ++dt)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const int e = dt * 32 + 8 * j + 4 * half;
+            if (kPart && e >= a.d) continue;
+            const float4 x = *reinterpret_cast<const float4*>(v + e);
+            const float y[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+            for (int c = 0; c < 4; ++c)
+              if (in && !(__builtin_fabsf(y[c]) < __builtin_inff())) o[dt][4 * j + c] += y[c];
+          }
+      }
+    }
+    leave_rows();
+  }
+
+  l = add_halves(l);
+  if (half == 0) {
+    join[(wave * 32 + col) * 2] = m;
+    join[(wave * 32 + col) * 2 + 1] = l;
+  }
+  __syncthreads();
+  float top = neg_inf(), sum = 0.f;
+#pragma unroll
+  for (int w = 0; w < 4; ++w) top = fmaxf(top, join[(w * 32 + col) * 2]);
+  const float base = top == neg_inf() ? 0.f : top;
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    const float* ml = join + (w * 32 + col) * 2;
+    sum = __builtin_fmaf(__builtin_amdgcn_exp2f(ml[0] - base), ml[1], sum);
+  }
+  float* part = reinterpret_cast<float*>(lds);                // [wave][D][32]
+  const float f = __builtin_amdgcn_exp2f(m - base);
+#pragma unroll
+  for (int dt = 0; dt < kCols; ++dt)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) part[(wave * D + dt * 32 + key_of(i)) * 32 + col] = o[dt][i] * f;
+  __syncthreads();
+  if (!mine) return;
+  for (int e = (threadIdx.x >> 5) * 4; e < a.d; e += 32) {
+    float y[4];
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+      y[c] = 0.f;
+#pragma unroll
+      for (int w = 0; w < 4; ++w) y[c] += part[(w * D + e + c) * 32 + col];
+    }
+    const float4 x = make_float4(y[0], y[1], y[2], y[3]);
+    if (a.splits > 1) store_result<0, true>(a, split, row, a.d, e, x, top, sum);
+    else store_result<0, false>(a, split, row, a.d, e, x, top, sum);
   }
 }
 
@@ -870,8 +979,8 @@ static __global__ __launch_bounds__(PAIR ? 512 : 256, 2) void k_attn_rows(AttnAr
         for (int w = 0; w < kRowWaves; ++w) y[c] += part[((first + w) * D + e + c) * 32 + col];
       }
       const float4 o = make_float4(y[0], y[1], y[2], y[3]);
-      if (a.splits > 1) store_result<true>(a, split, row, D, e, o, top, sum);
-      else store_result<false>(a, split, row, D, e, o, top, sum);
+      if (a.splits > 1) store_result<1, true>(a, split, row, D, e, o, top, sum);
+      else store_result<1, false>(a, split, row, D, e, o, top, sum);
     }
   }
 }
@@ -1197,8 +1306,8 @@ static __global__ __launch_bounds__(512, 2) void k_attn_chunk(AttnArgs a) {
     for (int j = 0; j < 4; ++j) {
       const int e = dt * 32 + 8 * j + 4 * half;
       const float4 o = make_float4(st[0].o[dt][4 * j], st[0].o[dt][4 * j + 1], st[0].o[dt][4 * j + 2], st[0].o[dt][4 * j + 3]);
-      if (a.splits > 1) store_result<true>(a, split, row, D, e, o, st[0].m, l);
-      else store_result<false>(a, split, row, D, e, o, st[0].m, l);
+      if (a.splits > 1) store_result<1, true>(a, split, row, D, e, o, st[0].m, l);
+      else store_result<1, false>(a, split, row, D, e, o, st[0].m, l);
     }
 }
 

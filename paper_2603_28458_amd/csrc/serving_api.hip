@@ -44,7 +44,7 @@ int check_attention(const hisa_queries* q, const hisa_cache* c, int32_t k) {
   if (c->page & (c->page - 1) || overflows31(c->max_pages, c->page)) return HISA_ERR_SHAPE;
   if (k < 0 || k > kMaxList) return HISA_ERR_SHAPE;
   if (q->q_dtype == HISA_F32 && c->dtype == HISA_F32) {
-    if (c->d < 4 || c->d % 4 || c->d > kPlainMaxD) return HISA_ERR_SHAPE;
+    if (c->d < 4 || c->d % 4 || c->d > kF32MaxD) return HISA_ERR_SHAPE;
   } else if (q->q_dtype == HISA_BF16 && (c->dtype == HISA_BF16 || c->dtype == HISA_FP8_E4M3)) {
     if (c->d != 64 && c->d != 128) return HISA_ERR_SHAPE;
   } else {
@@ -54,7 +54,7 @@ int check_attention(const hisa_queries* q, const hisa_cache* c, int32_t k) {
 }
 
 // How a call is cut into workgroups; the same answer for the workspace and for the launch.
-enum AttnKernel { ATTN_PLAIN, ATTN_ROWS, ATTN_CHUNK };
+enum AttnKernel { ATTN_F32, ATTN_ROWS, ATTN_CHUNK };
 struct AttnPlan {
   AttnKernel kernel;
   bool pair;          // ATTN_ROWS: 64 heads per workgroup, not 32
@@ -69,10 +69,10 @@ AttnPlan plan_attention(const hisa_queries* q, const hisa_cache* c, int32_t k) {
   const long G = q->H / c->H_kv, T = q->T;
   long most, want;
   if (c->dtype == HISA_F32) {
-    p.kernel = ATTN_PLAIN;
-    p.units = T * ((G + kPlainHeads - 1) / kPlainHeads);
-    most = (keys + 511) / 512;
-    want = 1024;
+    p.kernel = ATTN_F32;
+    p.units = k ? T * ((G + 31) / 32) : T * G / 32 + c->n_seq;
+    most = (keys + 127) / 128;
+    want = 512;
   } else if (k || T <= c->n_seq) {
     p.kernel = ATTN_ROWS;
     p.pair = G > 32;
@@ -146,6 +146,15 @@ int launch_mfma(const AttnArgs& a, const AttnPlan& p, dim3 grid, hipStream_t st)
   return HISA_OK;
 }
 
+template <int D, bool LIST>
+int launch_f32(const AttnArgs& a, dim3 grid, hipStream_t st) {
+  constexpr auto kern = k_attn_f32<D, LIST>;
+  constexpr int lds = F32Geom<D>::kLds;
+  if (lds > 65536 && raise_lds_limit<kern>(lds)) return HISA_ERR_LAUNCH;
+  hipLaunchKernelGGL(kern, grid, dim3(256), lds, st, a);
+  return HISA_OK;
+}
+
 template <bool LIST>
 int launch_attention(AttnArgs a, const AttnPlan& p, int dtype, hipStream_t st) {
   const long wgs = p.units * a.H_kv * a.splits;
@@ -153,7 +162,9 @@ int launch_attention(AttnArgs a, const AttnPlan& p, int dtype, hipStream_t st) {
   const dim3 grid((unsigned)wgs);
   int status = HISA_OK;
   if (dtype == HISA_F32)
-    hipLaunchKernelGGL((k_attn_plain<LIST>), grid, dim3(256), 0, st, a);
+    status = a.d == 64    ? launch_f32<64, LIST>(a, grid, st)
+             : a.d == 128 ? launch_f32<128, LIST>(a, grid, st)
+                          : launch_f32<kF32MaxD, LIST>(a, grid, st);
   else if (dtype == HISA_BF16)
     status = a.d == 128 ? launch_mfma<128, 1, LIST>(a, p, grid, st) : launch_mfma<64, 1, LIST>(a, p, grid, st);
   else
