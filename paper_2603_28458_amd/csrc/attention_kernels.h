@@ -1311,39 +1311,74 @@ static __global__ __launch_bounds__(512, 2) void k_attn_chunk(AttnArgs a) {
     }
 }
 
-// Joins the parts of a row: 4 columns per lane, rows of a token in consecutive groups of lanes.
+// Joins the parts of a row: 4 columns per lane, 8 parts asked for at once (what this costs is the way to memory, once per
+// 8 parts), `groups` sets of lanes per row that share its parts and meet in LDS.
+constexpr int kJoinParts = 8;
+
+struct Joined {
+  float4 o;
+  float m, l;
+};
+__device__ __forceinline__ void join_part(Joined& j, float f, float4 o, float l) {
+  j.l = __builtin_fmaf(f, l, j.l);
+  j.o.x = __builtin_fmaf(f, o.x, j.o.x);
+  j.o.y = __builtin_fmaf(f, o.y, j.o.y);
+  j.o.z = __builtin_fmaf(f, o.z, j.o.z);
+  j.o.w = __builtin_fmaf(f, o.w, j.o.w);
+}
+
 template <int QDT, bool LIST>
-static __global__ __launch_bounds__(256) void k_attn_join(AttnArgs a) {
-  const int per = a.d / 4;
-  const long i = (long)blockIdx.x * 256 + threadIdx.x;
-  const long r = i / per;
-  const int e = (int)(i - r * per) * 4;
-  if (r >= (long)a.T * a.H) return;
+static __global__ __launch_bounds__(256) void k_attn_join(AttnArgs a, int groups) {
+  __shared__ float4 group_o[256];
+  __shared__ float2 group_ml[256];
+  const int per = a.d / 4, rows = 256 / per / groups;         // lanes of a set, rows of this workgroup
+  const int set = threadIdx.x / per, e = (threadIdx.x - set * per) * 4, group = set % groups;
+  const long r = (long)blockIdx.x * rows + set / groups, all = (long)a.T * a.H;
+  bool mine = set < rows * groups && r < all;
   if constexpr (!LIST) {
     const int t = (int)(r / a.H);
-    if (t < a.q_start[0] || t >= a.q_start[a.n_seq]) return;
+    mine = mine && t >= a.q_start[0] && t < a.q_start[a.n_seq];
   }
-  const float* ml = a.part + (long)a.splits * a.T * a.H * a.d;
-  float top = neg_inf();
-  for (int s = 0; s < a.splits; ++s) top = fmaxf(top, ml[((long)s * a.T * a.H + r) * 2]);
-  const float base = top == neg_inf() ? 0.f : top;
-  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-  float sum = 0.f;
-  for (int s = 0; s < a.splits; ++s) {
-    const long pr = (long)s * a.T * a.H + r;
-    const float l = ml[pr * 2 + 1];
-    if (l == 0.f) continue;
-    const float f = __builtin_amdgcn_exp2f(ml[pr * 2] - base);
-    sum = __builtin_fmaf(f, l, sum);
-    const float4 x = *reinterpret_cast<const float4*>(a.part + pr * a.d + e);
-    o.x = __builtin_fmaf(f, x.x, o.x);
-    o.y = __builtin_fmaf(f, x.y, o.y);
-    o.z = __builtin_fmaf(f, x.z, o.z);
-    o.w = __builtin_fmaf(f, x.w, o.w);
+  Joined j{make_float4(0.f, 0.f, 0.f, 0.f), neg_inf(), 0.f};
+  if (mine) {
+    const float2* ml = reinterpret_cast<const float2*>(a.part + a.splits * all * a.d);
+    for (int first = group * kJoinParts; first < a.splits; first += groups * kJoinParts) {
+      float2 x[kJoinParts];
+      float4 o[kJoinParts];
+#pragma unroll
+      for (int i = 0; i < kJoinParts; ++i) {
+        const long pr = (first + i < a.splits ? first + i : a.splits - 1) * all + r;
+        x[i] = ml[pr];
+        o[i] = *reinterpret_cast<const float4*>(a.part + pr * a.d + e);
+      }
+      float top = j.m;
+#pragma unroll
+      for (int i = 0; i < kJoinParts; ++i) top = fmaxf(top, x[i].x);
+      const float base = top == neg_inf() ? 0.f : top, f = __builtin_amdgcn_exp2f(j.m - base);
+      j = Joined{make_float4(j.o.x * f, j.o.y * f, j.o.z * f, j.o.w * f), top, j.l * f};
+#pragma unroll
+      for (int i = 0; i < kJoinParts; ++i)
+        if (first + i < a.splits) join_part(j, __builtin_amdgcn_exp2f(x[i].x - base), o[i], x[i].y);
+    }
   }
-  const float inv = sum == 0.f ? 0.f : 1.f / sum;
-  store_four<QDT>(a, r, e, make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv));
-  if (e == 0 && a.lse) a.lse[r] = sum == 0.f ? neg_inf() : (base + log2f(sum)) * 0.693147180559945309f;
+  if (groups > 1) {
+    group_o[threadIdx.x] = j.o;
+    group_ml[threadIdx.x] = make_float2(j.m, j.l);
+    __syncthreads();
+    if (group != 0) return;
+    float top = j.m;
+    for (int g = 1; g < groups && mine; ++g) top = fmaxf(top, group_ml[threadIdx.x + g * per].x);
+    const float base = top == neg_inf() ? 0.f : top, f = __builtin_amdgcn_exp2f(j.m - base);
+    j = Joined{make_float4(j.o.x * f, j.o.y * f, j.o.z * f, j.o.w * f), top, j.l * f};
+    for (int g = 1; g < groups && mine; ++g) {
+      const float2 x = group_ml[threadIdx.x + g * per];
+      join_part(j, __builtin_amdgcn_exp2f(x.x - base), group_o[threadIdx.x + g * per], x.y);
+    }
+  }
+  if (!mine) return;
+  const float inv = j.l == 0.f ? 0.f : 1.f / j.l;
+  store_four<QDT>(a, r, e, make_float4(j.o.x * inv, j.o.y * inv, j.o.z * inv, j.o.w * inv));
+  if (e == 0 && a.lse) a.lse[r] = j.l == 0.f ? neg_inf() : (j.m + log2f(j.l)) * 0.693147180559945309f;
 }
 
 }  // namespace hisa

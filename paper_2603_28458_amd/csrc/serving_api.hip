@@ -171,11 +171,16 @@ int launch_attention(AttnArgs a, const AttnPlan& p, int dtype, hipStream_t st) {
     status = a.d == 128 ? launch_mfma<128, 2, LIST>(a, p, grid, st) : launch_mfma<64, 2, LIST>(a, p, grid, st);
   if (status) return status;
   if (a.splits > 1) {
-    const dim3 jg((unsigned)(((long)a.T * a.H * (a.d / 4) + 255) / 256));
+    // more sets of lanes per row while that spares a trip to memory and the workgroup has them
+    const int sets = 256 / (a.d / 4);
+    int groups = 1;
+    while (groups * 2 <= sets && groups * kJoinParts < a.splits) groups *= 2;
+    const int rows = sets / groups;
+    const dim3 jg((unsigned)(((long)a.T * a.H + rows - 1) / rows));
     if (dtype == HISA_F32)
-      hipLaunchKernelGGL((k_attn_join<0, LIST>), jg, dim3(256), 0, st, a);
+      hipLaunchKernelGGL((k_attn_join<0, LIST>), jg, dim3(256), 0, st, a, groups);
     else
-      hipLaunchKernelGGL((k_attn_join<1, LIST>), jg, dim3(256), 0, st, a);
+      hipLaunchKernelGGL((k_attn_join<1, LIST>), jg, dim3(256), 0, st, a, groups);
   }
   return launch_status();
 }
