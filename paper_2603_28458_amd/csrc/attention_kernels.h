@@ -1017,12 +1017,12 @@ struct ChunkGeom {
   static constexpr int kLds = kRings + 8 * kChunkKeys * 16 + 8 * 8 + 8 * 4 + (KDT == 2 ? 8 * 2 * kChunkKeys * 4 : 0);
 };
 
-// 16 or 4 bytes per lane from `src` to LDS byte lds + 16 (or 4) * lane.
+// 16 or 4 bytes per lane from `src` to LDS byte lds + 16 (or 4) * lane.  (Nothing else here has a use for m0.)
 __device__ __forceinline__ void dma16(uint32_t lds, const void* src) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds), "v"(src) : "memory");
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(__builtin_amdgcn_readfirstlane((int)lds)), "v"(src) : "memory");
 }
 __device__ __forceinline__ void dma4(uint32_t lds, const void* src) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(lds), "v"(src) : "memory");
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(__builtin_amdgcn_readfirstlane((int)lds)), "v"(src) : "memory");
 }
 template <int N>
 __device__ __forceinline__ void dma_left() {   // until at most N requests of this wave are under way
@@ -1226,6 +1226,38 @@ static __global__ __launch_bounds__(512, 2) void k_attn_chunk(AttnArgs a) {
   finish(begin + 1, after(r), after(r), mask_of(begin + 1), mask_of(begin));
   if (group == 1) request(begin + 2 + (KDT == 2), where(begin + 2 + (KDT == 2)), KDT == 2 ? r : after(after(r)), 0);
   lds_barrier();
+  if (__builtin_amdgcn_readfirstlane(r0 + wave * 32 >= rows)) {
+    // A wave without rows goes through the loop below for its share of the tiles alone and leaves the others the machine.
+    if (group == 1) lds_barrier();
+    if (KDT == 2 && group == 1) finish(begin + 2, after(after(r)), after(after(r)), mask_of(begin + 2), mask_of(begin + 1));
+    // (the pages of later tiles are wave 0's business, which has rows)
+    auto bring = [&](int tile, int to) { request(tile, where(tile), KDT == 2 ? to : tile & 3, 0); };
+    bring(begin + group + 2 + (KDT == 2), group == 1 ? after(r) : r);
+    if (group == 0) lds_barrier();
+    for (int tile = begin; tile < end; ++tile) {
+      const int r1 = after(r), r2 = after(r1);
+      const uint64_t km = mask_of(tile + 2), vm = mask_of(tile + 1);
+      if (KDT == 1 && group == 1) {
+        step_arrived();
+        finish(tile + 2, r2, 0, km, vm);
+      }
+      if (group == 1) lds_barrier();
+      if constexpr (KDT == 2) {
+        step_arrived();
+        if (group == 0) finish(tile + 2, r2, r2, km, vm);
+        else finish(tile + 3, r, r, mask_of(tile + 3), km);
+      }
+      bring(tile + 3 + group + (KDT == 2), group == 0 ? r1 : r2);
+      if (KDT == 1 && group == 0) {
+        step_arrived();
+        finish(tile + 2, r2, 0, km, vm);
+      }
+      if (group == 0) lds_barrier();
+      r = r1;
+    }
+    dma_left<0>();
+    return;
+  }
   f32x16 s[1][2];
   bf16x8 p[1][4];
   if (group == 1) lds_barrier();

@@ -53,7 +53,8 @@ int check_attention(const hisa_queries* q, const hisa_cache* c, int32_t k) {
   return HISA_OK;
 }
 
-// How a call is cut into workgroups; the same answer for the workspace and for the launch.
+// How a call is cut into workgroups; the same answer for the workspace and for the launch.  (Times: H = 64, H_kv = 8,
+// d = 128, bf16 where nothing else is said.)
 enum AttnKernel { ATTN_F32, ATTN_ROWS, ATTN_CHUNK };
 struct AttnPlan {
   AttnKernel kernel;
@@ -63,31 +64,52 @@ struct AttnPlan {
   size_t ws_bytes;
 };
 
+constexpr long kCus = 256, kPartKeys = 256;
+
 AttnPlan plan_attention(const hisa_queries* q, const hisa_cache* c, int32_t k) {
   AttnPlan p{};
   const long keys = k ? k : (long)c->max_pages * c->page;
   const long G = q->H / c->H_kv, T = q->T;
-  long most, want;
+  long most = (keys + kPartKeys - 1) / kPartKeys, splits;
+  // A few new tokens a sequence: one at a time reads their keys that many times, from L2 for the most part, with every
+  // wave on keys of its own; together they read them once, but 32 rows are one wave's, and a tile of 64 keys takes it
+  // 4000 cycles from scores to values.  Measured, 64 sequences of 3000, 2 new tokens each: 145 us one at a time, 200
+  // together; 32 of 8000, 4 each: 290 and 323, fp8 220 and 420; 6 each: 354 and 340.  Wide groups fill the tile: 64 heads
+  // on one KV head, 64 sequences of 8000, 2 each: 119 and 97.
+  const long few = G > 32 ? 1 : c->dtype == HISA_FP8_E4M3 ? 4 : 2;
   if (c->dtype == HISA_F32) {
     p.kernel = ATTN_F32;
     p.units = k ? T * ((G + 31) / 32) : T * G / 32 + c->n_seq;
+    const long wgs = p.units * c->H_kv;
     most = (keys + 127) / 128;
-    want = 512;
-  } else if (k || T <= c->n_seq) {
+    splits = wgs < 2 * kCus ? 2 * kCus / wgs : 1;          // two workgroups per CU
+  } else if (k || T <= few * c->n_seq) {
     p.kernel = ATTN_ROWS;
+    // (one gathering of the keys for up to 64 heads: lists of 2048, 64 heads on one KV head, 1024 queries 155 us, two
+    // workgroups of 32 heads each 212)
     p.pair = G > 32;
     const long heads = p.pair ? 64 : 32;
     p.units = T * ((G + heads - 1) / heads);
-    most = (keys + 255) / 256;
-    want = k ? 512 : 2048;
+    // Two workgroups fit a CU, one with PAIR.  Over ranges four rounds of them even out sequences of different lengths (200
+    // sequences, 4 KV heads, fp8: 2 parts 468 us, 3 parts 490); lists are alike, and every part more is one more to join (100
+    // lists of 2048: 5 parts 41 us, 6 parts 48).
+    const long wgs = p.units * c->H_kv, want = k ? 2 * kCus : 8 * kCus;
+    splits = wgs < want ? want / wgs : 1;
   } else {
     p.kernel = ATTN_CHUNK;
     p.units = T * G / kChunkRows + c->n_seq;
-    most = (keys + 255) / 256;
-    want = 256;
+    // One workgroup per CU: the parts with which the last one is done first, if all sequences were alike; a part costs as
+    // much as 512 keys before and after its tiles.  (10 sequences of 5000, 30 new tokens each: 3 parts 75 us, 2 parts 91;
+    // one of 3000 with 700: 4 parts 110 us, 2 parts 137.)
+    const long each = (T * G + (long)c->n_seq * kChunkRows - 1) / ((long)c->n_seq * kChunkRows);
+    const long busy = each * c->n_seq * c->H_kv;
+    long best = 0;
+    splits = 1;
+    for (long s = 1; s <= most && (s == 1 || busy * s <= 4 * kCus); ++s) {
+      const long cost = (busy * s + kCus - 1) / kCus * ((keys + s - 1) / s + 512);
+      if (s == 1 || cost < best) best = cost, splits = s;
+    }
   }
-  const long wgs = p.units * c->H_kv;
-  long splits = (want + wgs - 1) / wgs;
   if (splits > most) splits = most;
   p.splits = (int)splits;
   p.ws_bytes = splits > 1 ? (size_t)splits * T * q->H * (c->d + 2) * 4 : 0;
