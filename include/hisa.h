@@ -329,9 +329,9 @@ int hisa_cache_append(const hisa_cache* cache, const int32_t* slots, const void*
  * d <= 256.  H <= 256, H_kv divides H; page a power of two; k, v and q 16-byte aligned, strides times
  * the element size multiples of 16 bytes; max_pages * page and n_pages * page below 2^31;
  * scale positive and finite.
- * Scores, the running maximum and sum and the output are held in fp32; the weights p_s are rounded to
- * bf16 for the second product (bf16 and fp8 caches).  All sums have a fixed order: the same call gives
- * the same bits.
+ * Scores, the running maximum and sum and the output are held in fp32; for the second product (bf16 and
+ * fp8 caches) the weights p_s are rounded to bf16, where T * H <= 1024 to two bf16 parts (16 bits).  All
+ * sums have a fixed order: the same call gives the same bits.
  * Workspace: hisa_attention_workspace_bytes(queries, cache, 0), which depends on shapes only.
  */
 int hisa_paged_attention(const hisa_queries* queries, const hisa_cache* cache, const int32_t* q_start,

@@ -221,9 +221,16 @@ __device__ __forceinline__ void scale_scores(f32x16 (&s)[NB], const float* ks) {
 }
 
 // Scores of NB blocks of 32 keys -> weights as B operands; updates m, l, o.  vs: scales of the value rows (fp8).
-template <int D, int KDT, int NB>
-__device__ __forceinline__ void softmax_tile(RowState<D>& st, const f32x16 (&s)[NB], bf16x8 (&p)[2 * NB], float c,
-                                             const float* vs) {
+// A weight rounded to bf16 is off by up to 2^-8 of itself (1.6e-3 in the mean square), and so are the sums: as much as the
+// result's own rounding adds.  REST: what is left of each weight goes to `rest`, for a second product of the values,
+// with which the sums are as good as with weights in fp32 (to 2^-16).  It is cut and not rounded off, so that both parts have
+// one sign, and never 0 where there is a weight: an infinite value stays what it is in both products.
+__device__ __forceinline__ float cut_off(float w, uint32_t bits) {
+  return __builtin_amdgcn_fmed3f(w - __uint_as_float(bits & 0xffff0000u), w, 1.17549435e-38f);
+}
+template <int D, int KDT, int NB, bool REST>
+__device__ __forceinline__ void softmax_tile(RowState<D>& st, const f32x16 (&s)[NB], bf16x8 (&p)[2 * NB],
+                                             bf16x8 (&rest)[2 * NB], float c, const float* vs) {
   const int half = lane_id() >> 5;
   // (the IEEE 754-2019 maximum: three operands an instruction, none of them quieted first as fmaxf's are; a NaN comes
   // through it, leaves m as it is and makes the row's sum NaN below)
@@ -269,22 +276,33 @@ __device__ __forceinline__ void softmax_tile(RowState<D>& st, const f32x16 (&s)[
         w[3] *= f.w;
       }
 #pragma unroll
-      for (int e = 0; e < 4; ++e) p[2 * b + (j >> 1)][4 * (j & 1) + e] = (__bf16)w[e];
+      for (int e = 0; e < 4; e += 2) {
+        const int at = 4 * (j & 1) + e;
+        bf16x2 first = {(__bf16)w[e], (__bf16)w[e + 1]};
+        if constexpr (REST) {
+          const uint32_t x = __float_as_uint(w[e]), y = __float_as_uint(w[e + 1]);
+          first = __builtin_bit_cast(bf16x2, (y & 0xffff0000u) | x >> 16);
+          rest[2 * b + (j >> 1)][at] = (__bf16)cut_off(w[e], x);
+          rest[2 * b + (j >> 1)][at + 1] = (__bf16)cut_off(w[e + 1], y);
+        }
+        p[2 * b + (j >> 1)][at] = first[0];
+        p[2 * b + (j >> 1)][at + 1] = first[1];
+      }
     }
   st.l += sum0 + sum1;
 }
 
-// O^T += V^T P^T over NB blocks of 32 keys.
-template <int D, int NB, int NQ>
-__device__ __forceinline__ void add_values(RowState<D> (&st)[NQ], const unsigned char* tile, int read_value,
-                                           const bf16x8 (&p)[NQ][2 * NB]) {
+// O^T += V^T P^T over 32 keys.
+template <int D, bool REST>
+__device__ __forceinline__ void add_values(RowState<D>& st, const unsigned char* tile, int read_value, const bf16x8 (&p)[2],
+                                           const bf16x8 (&rest)[2]) {
 #pragma unroll
   for (int dt = 0; dt < D / 32; ++dt)
 #pragma unroll
-    for (int kk = 0; kk < 2 * NB; ++kk) {
+    for (int kk = 0; kk < 2; ++kk) {
       const bf16x8 v = RowTile<D>::value_operand(tile, read_value, 16 * kk, dt);
-#pragma unroll
-      for (int n = 0; n < NQ; ++n) st[n].o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, p[n][kk], st[n].o[dt], 0, 0, 0);
+      st.o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, p[kk], st.o[dt], 0, 0, 0);
+      if constexpr (REST) st.o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, rest[kk], st.o[dt], 0, 0, 0);
     }
 }
 
@@ -358,10 +376,10 @@ __device__ __forceinline__ void score_tile(const RowState<D> (&st)[NQ], const un
 // eight are under way from LDS while one is multiplied: the order is pinned, because the compiler's own asks for four at
 // most and the matrix unit then waits for LDS after every second product.  Consecutive products have different
 // accumulators.
-template <int D, class Between>
+template <int D, bool REST, class Between>
 __device__ __forceinline__ void products(RowState<D>& st, const unsigned char* kt, int read_key, f32x16 (&s)[2],
                                          const unsigned char* vt, int read_value, const bf16x8 (&p)[4],
-                                         Between between) {
+                                         const bf16x8 (&rest)[4], Between between) {
   constexpr int kAhead = 6, kScores = D / 8, kTiles = D / 32;
   bf16x8 f[kAhead];
   auto operand = [&](int i) {
@@ -383,6 +401,8 @@ __device__ __forceinline__ void products(RowState<D>& st, const unsigned char* k
     } else {
       const int j = i - kScores;
       st.o[j % kTiles] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, p[j / kTiles], st.o[j % kTiles], 0, 0, 0);
+      if constexpr (REST)
+        st.o[j % kTiles] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, rest[j / kTiles], st.o[j % kTiles], 0, 0, 0);
     }
     if (i + kAhead < 2 * kScores) f[i % kAhead] = operand(i + kAhead);
     between(i);
@@ -763,7 +783,7 @@ struct RowGeom {
   static constexpr int kLds = kJoin + kWaves * 256;
 };
 
-template <int D, int KDT, bool PAIR, bool LIST>
+template <int D, int KDT, bool PAIR, bool LIST, bool REST>
 static __global__ __launch_bounds__(PAIR ? 512 : 256, 2) void k_attn_rows(AttnArgs a) {
   using Geo = RowGeom<D, KDT, PAIR>;
   extern __shared__ __align__(16) unsigned char lds[];
@@ -916,15 +936,15 @@ static __global__ __launch_bounds__(PAIR ? 512 : 256, 2) void k_attn_rows(AttnAr
     s_after = position(tile + (Geo::kDepth + 2) * kRowWaves);
     if (!PAIR || tile < end) {
       f32x16 s[1][1];
-      bf16x8 p[1][2];
+      bf16x8 p[1][2], rest[1][2];
       score_tile<D, 1, 1>(st, kt, renewed(read_key), s);
       if constexpr (KDT == 2) scale_scores<1>(s[0], sc);
       if (keys != 0xffffffffu) {
         asm volatile("");                       // (a branch, not selects for every tile)
         hide_keys(s[0][0], keys);
       }
-      softmax_tile<D, KDT, 1>(st[0], s[0], p[0], a.scale_log2, sc + 32);
-      add_values<D, 1, 1>(st, vt, renewed(read_value), p);
+      softmax_tile<D, KDT, 1, REST>(st[0], s[0], p[0], rest[0], a.scale_log2, sc + 32);
+      add_values<D, REST>(st[0], vt, renewed(read_value), p[0], rest[0]);
     }
     if constexpr (!PAIR) wave_lds_order();
     tile += kRowWaves;
@@ -1029,7 +1049,7 @@ __device__ __forceinline__ void dma_left() {   // until at most N requests of th
   asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
 }
 
-template <int D, int KDT>
+template <int D, int KDT, bool REST>
 static __global__ __launch_bounds__(512, 2) void k_attn_chunk(AttnArgs a) {
   using Geo = ChunkGeom<D, KDT>;
   extern __shared__ __align__(16) unsigned char lds[];
@@ -1259,7 +1279,7 @@ static __global__ __launch_bounds__(512, 2) void k_attn_chunk(AttnArgs a) {
     return;
   }
   f32x16 s[1][2];
-  bf16x8 p[1][4];
+  bf16x8 p[1][4], rest[4];
   if (group == 1) lds_barrier();
   score_tile<D, 2, 1>(st, lds + key_tile(r), renewed(read_key), s);
   {
@@ -1282,11 +1302,14 @@ static __global__ __launch_bounds__(512, 2) void k_attn_chunk(AttnArgs a) {
         hide(st[0], s[0][0], (uint32_t)mask, base);
         hide(st[0], s[0][1], (uint32_t)(mask >> 32), base + 32);
       }
-      softmax_tile<D, KDT, 2>(st[0], s[0], p[0], a.scale_log2, sc + kChunkKeys);
+      softmax_tile<D, KDT, 2, REST>(st[0], s[0], p[0], rest, a.scale_log2, sc + kChunkKeys);
     }
     // (the weights are made here and not, as the compiler would have it, between the products that need them)
 #pragma unroll
     for (int i = 0; i < 4; ++i) asm volatile("" : "+v"(p[0][i]));
+    if constexpr (REST)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) asm volatile("" : "+v"(rest[i]));
     asm volatile("" : "+v"(st[0].l));
     if (wave == 0) publish(tile + 5, pages[((tile + 5) & 7) * kChunkKeys + lane]);
     if (group == 1) {
@@ -1309,7 +1332,7 @@ static __global__ __launch_bounds__(512, 2) void k_attn_chunk(AttnArgs a) {
     Where at;
     constexpr int kProducts = D / 4;
     __builtin_amdgcn_s_setprio(3);           // (the wave that multiplies goes first: 0.5 % at 1024 new tokens behind 64K)
-    products<D>(st[0], lds + key_tile(r1), renewed(read_key), s[0], lds + value_tile(r), renewed(read_value), p[0], [&](int i) {
+    products<D, REST>(st[0], lds + key_tile(r1), renewed(read_key), s[0], lds + value_tile(r), renewed(read_value), p[0], rest, [&](int i) {
       if (i == 1) at = where(asked);
       // (fp8: the buffer of the step before the one that is widened now)
       if (i == kProducts / 4) request(asked, at, KDT == 2 ? (group == 0 ? r1 : r2) : asked & 3, tile + 7 + (KDT == 2));

@@ -59,6 +59,7 @@ enum AttnKernel { ATTN_F32, ATTN_ROWS, ATTN_CHUNK };
 struct AttnPlan {
   AttnKernel kernel;
   bool pair;          // ATTN_ROWS: 64 heads per workgroup, not 32
+  bool rest;          // bf16, fp8: weights in two parts
   long units;         // tiles of query rows, of one KV head
   int splits;         // parts of their keys
   size_t ws_bytes;
@@ -71,6 +72,11 @@ AttnPlan plan_attention(const hisa_queries* q, const hisa_cache* c, int32_t k) {
   const long keys = k ? k : (long)c->max_pages * c->page;
   const long G = q->H / c->H_kv, T = q->T;
   long most = (keys + kPartKeys - 1) / kPartKeys, splits;
+  // Weights to 16 bits and not to 8 where there are few rows: rounding errors of random sign do not average out over those
+  // (the mean square error of 7 rows was up to 1.7 times that of a rounded result, of 1024 rows 1.45 times; with it 1.00),
+  // and such a call waits for other things than the second product (one token over 130K keys 115 and 116 us, 16 lists of
+  // 2048 15.6 and 16.1).  With many rows it costs what a product costs (1024 lists of 2048 145 and 163 us).
+  p.rest = T * q->H <= 1024;
   // A few new tokens a sequence: one at a time reads their keys that many times, from L2 for the most part, with every
   // wave on keys of its own; together they read them once, but 32 rows are one wave's, and a tile of 64 keys takes it
   // 4000 cycles from scores to values.  Measured, 64 sequences of 3000, 2 new tokens each: 145 us one at a time, 200
@@ -146,26 +152,31 @@ AttnArgs attention_args(const hisa_queries* q, const hisa_cache* c, float scale,
   return a;
 }
 
-template <int D, int KDT, bool PAIR, bool LIST>
+template <int D, int KDT, bool PAIR, bool LIST, bool REST>
 int launch_rows(const AttnArgs& a, dim3 grid, hipStream_t st) {
   using Geo = RowGeom<D, KDT, PAIR>;
-  constexpr auto kern = k_attn_rows<D, KDT, PAIR, LIST>;
+  constexpr auto kern = k_attn_rows<D, KDT, PAIR, LIST, REST>;
   if (Geo::kLds > 65536 && raise_lds_limit<kern>(Geo::kLds)) return HISA_ERR_LAUNCH;
   hipLaunchKernelGGL(kern, grid, dim3(64 * Geo::kWaves), Geo::kLds, st, a);
   return HISA_OK;
 }
 
-template <int D, int KDT, bool LIST>
-int launch_mfma(const AttnArgs& a, const AttnPlan& p, dim3 grid, hipStream_t st) {
+template <int D, int KDT, bool LIST, bool REST>
+int launch_parts(const AttnArgs& a, const AttnPlan& p, dim3 grid, hipStream_t st) {
   if (p.kernel == ATTN_ROWS)
-    return p.pair ? launch_rows<D, KDT, true, LIST>(a, grid, st) : launch_rows<D, KDT, false, LIST>(a, grid, st);
+    return p.pair ? launch_rows<D, KDT, true, LIST, REST>(a, grid, st) : launch_rows<D, KDT, false, LIST, REST>(a, grid, st);
   if constexpr (!LIST) {
-    constexpr auto kern = k_attn_chunk<D, KDT>;
+    constexpr auto kern = k_attn_chunk<D, KDT, REST>;
     constexpr int lds = ChunkGeom<D, KDT>::kLds;
     if (lds > 65536 && raise_lds_limit<kern>(lds)) return HISA_ERR_LAUNCH;
     hipLaunchKernelGGL(kern, grid, dim3(64 * kChunkWaves), lds, st, a);
   }
   return HISA_OK;
+}
+
+template <int D, int KDT, bool LIST>
+int launch_mfma(const AttnArgs& a, const AttnPlan& p, dim3 grid, hipStream_t st) {
+  return p.rest ? launch_parts<D, KDT, LIST, true>(a, p, grid, st) : launch_parts<D, KDT, LIST, false>(a, p, grid, st);
 }
 
 template <int D, bool LIST>
