@@ -247,8 +247,9 @@ __device__ __forceinline__ void softmax_tile(RowState<D>& st, const f32x16 (&s)[
   }
   float top = __builtin_elementwise_maximum(__builtin_elementwise_maximum(top4[0], top4[1]), top4[2]);
   top = max_halves(__builtin_elementwise_maximum(top, top4[3])) * c;
-  if (__builtin_amdgcn_ballot_w64(top > st.m + kSlack)) {
-    const float mn = fmaxf(st.m, top);
+  const bool grown = top > st.m + kSlack;
+  if (__builtin_amdgcn_ballot_w64(grown)) {
+    const float mn = grown ? top : st.m;     // (a row goes by its own scores, not by its neighbours')
     const float f = __builtin_amdgcn_exp2f(st.m - (mn == neg_inf() ? 0.f : mn));
     st.m = mn;
     st.l *= f;
@@ -658,8 +659,9 @@ static __global__ __launch_bounds__(256, D > 128 ? 1 : 2) void k_attn_f32(AttnAr
       top = __builtin_elementwise_maximum(top, s[i]);
     }
     top = max_halves(top);
-    if (__builtin_amdgcn_ballot_w64(top > m + kSlack)) {
-      const float mn = fmaxf(m, top);
+    const bool grown = top > m + kSlack;
+    if (__builtin_amdgcn_ballot_w64(grown)) {
+      const float mn = grown ? top : m;
       const float f = __builtin_amdgcn_exp2f(m - (mn == neg_inf() ? 0.f : mn));
       m = mn;
       l *= f;

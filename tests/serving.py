@@ -7,7 +7,8 @@ Tolerances, from the arithmetic (u = half a step of the output type relative to 
   scores    dot products of d terms in fp32 are off by at most (d + 8) * 2^-24 * sum |q k|, which shifts a weight by
             that much, times the scale, relatively: E (the largest over the batch, plus 2^-19 for the exponential of an
             fp32 argument of magnitude up to 2^6);
-  weights   rounded to bf16 for the second product: 2^-8 each (bf16 and fp8 caches), nothing in fp32;
+  weights   rounded to bf16 for the second product: 2^-8 each (bf16 and fp8 caches), nothing in fp32.  In two parts the
+            first is cut (off by 2^-7 at most) and the second, what is left, rounded to bf16: 2^-7 2^-8 = 2^-15 each;
   sums      n terms in fp32 in any order: n * 2^-24, at most 2^-11 for n <= 8192, of sum p |v| / sum p = mag; this
             is far above what a tree or a matrix unit makes of it, so a quarter of it is asked for;
   output    u * |out|.
@@ -122,13 +123,13 @@ class Batch:
         return SO.attention(self.q64, self.rows64["k"], self.rows64["v"], self.table, self.seq_len, self.page, seq_of,
                             positions_of, scale)
 
-    def check(self, got, lse, want, n_max, scale=None, what=""):
+    def check(self, got, lse, want, n_max, scale=None, what="", weights=2.0 ** -8):
         out, wlse, mag = want
         scale = self.d ** -0.5 if scale is None else scale
         kmax = np.nanmax(np.where(np.isfinite(self.rows64["k"]), np.abs(self.rows64["k"]), 0).sum(axis=2))
         E = (self.d + 8) * 2.0 ** -24 * scale * np.abs(self.q64).max() * kmax + 2.0 ** -19
         u = 2.0 ** -24 if self.kv == "f32" else 2.0 ** -8
-        w = 0.0 if self.kv == "f32" else 2.0 ** -8
+        w = 0.0 if self.kv == "f32" else weights
         g = f64(got)
         mine = ~np.isnan(wlse)                                       # (rows that are somebody's)
         rel = 2 * E + w + n_max * 2.0 ** -26 + 2.0 ** -20

@@ -1,0 +1,101 @@
+"""The attention calls on either side of the sizes at which they take another way: weights in one or two parts, one token at
+a time or tiles of rows, many parts to join, waves without rows, fp32 heads of any number and size."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2603_28458_amd import hisa
+from tests import test_paged_attention_gpu as paged
+from tests import test_sparse_attention_gpu as sparse
+from tests.serving import Batch
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("kv", ["bf16", "fp8"])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("lens,H,H_kv", [([(40, 1)], 7, 1), ([(700, 1), (64, 1)], 8, 2), ([(2000, 1)], 64, 1),
+                                         ([(300, 9), (20, 30)], 8, 2), ([(0, 8)], 128, 2)])
+def test_few_rows_are_as_good_as_their_own_rounding(kv, d, lens, H, H_kv):
+    b = Batch(lens, H=H, H_kv=H_kv, d=d, kv=kv, seed=H + d)
+    assert b.T * H <= 1024
+    b.queries.q_pos = b.put(b.pos)
+    out, lse = hisa.hisa_paged_attention(b.queries, b.cache, b.q_start, want_lse=True)
+    want = b.want(lambda t: np.arange(int(b.pos[t]) + 1))
+    b.check(out, lse, want, int(b.seq_len.max()), what="few rows", weights=2.0 ** -15)
+    k = int(b.seq_len.max())
+    lists = sparse.draw(b, k, 1)                                     # (all positions that a query sees)
+    out, lse = hisa.hisa_sparse_attention(b.queries, b.cache, b.put(lists), want_lse=True)
+    b.check(out, lse, want, k, what="few lists", weights=2.0 ** -15)
+
+
+@pytest.mark.parametrize("kv", ["bf16", "fp8", "f32"])
+@pytest.mark.parametrize("tokens", [2, 3, 4, 5, 8, 9, 33])
+@pytest.mark.parametrize("H,H_kv", [(8, 2), (64, 1), (40, 8)])
+def test_a_few_new_tokens(kv, tokens, H, H_kv):
+    """T at and around two, four tokens a sequence, lengths unequal; T * H on both sides of 1024."""
+    b = Batch([(90, tokens), (513, 1), (0, tokens), (31, 0), (5, 2)], H=H, H_kv=H_kv, kv=kv, seed=tokens)
+    paged.run(b, what=f"{tokens} tokens")
+    paged.run(b, lo=np.maximum(0, b.pos - 40), what=f"{tokens} tokens, windows")
+
+
+@pytest.mark.parametrize("kv,d,H,H_kv", [("bf16", 128, 8, 8), ("fp8", 64, 8, 1), ("bf16", 64, 64, 1), ("f32", 128, 8, 2),
+                                         ("f32", 20, 3, 1), ("f32", 64, 4, 4), ("f32", 256, 2, 1)])
+def test_many_parts_of_one_row(kv, d, H, H_kv):
+    """One token over a long sequence beside a short one: up to 256 parts of the long row, most of the short one's empty."""
+    b = Batch([(33000, 1), (70, 1)], H=H, H_kv=H_kv, d=d, kv=kv, page=64, seed=d, q_gain=1.0)
+    paged.run(b, what="parts")
+    b = Batch([(9000, 70)], H=H, H_kv=H_kv, d=d, kv=kv, page=64, seed=d + 1, q_gain=1.0)
+    paged.run(b, what="parts of a chunk")
+
+
+@pytest.mark.parametrize("k", [2048, 9000])
+@pytest.mark.parametrize("kv", ["bf16", "fp8", "f32"])
+def test_many_parts_of_one_list(kv, k):
+    b = Batch([(9500, 1), (100, 1)], H=16, H_kv=1, kv=kv, page=64, seed=k, q_gain=1.0)
+    sparse.run(b, sparse.draw(b, k, 5, holes=0.1), what="parts")
+
+
+@pytest.mark.parametrize("kv", ["bf16", "f32"])
+@pytest.mark.parametrize("new,H", [(1, 4), (1, 128), (9, 8), (9, 128), (70, 2), (70, 32), (300, 8)])
+def test_infinite_values_stay_what_they_are(kv, new, H):
+    b = Batch([(40, new)], H=H, H_kv=1 if H < 128 else 2, kv=kv, seed=new)
+    page, o = int(b.table[0, 40 // b.page]), 40 % b.page
+    for e, x in ((3, float("inf")), (4, -float("inf")), (5, float("nan"))):
+        b.cache.v[page, o, :, e] = x
+    b.queries.q_pos = b.put(b.pos)
+    lists = b.put(np.tile(np.arange(41, dtype=np.int32), (b.T, 1)))
+    for out, _ in (hisa.hisa_paged_attention(b.queries, b.cache, b.q_start),
+                   hisa.hisa_sparse_attention(b.queries, b.cache, lists)):
+        assert (out[:, :, 3] == float("inf")).all() and (out[:, :, 4] == -float("inf")).all()
+        assert out[:, :, 5].isnan().all()
+        assert out[:, :, 6:].isfinite().all() and out[:, :, :3].isfinite().all()
+
+
+@pytest.mark.parametrize("kv", ["bf16", "fp8", "f32"])
+@pytest.mark.parametrize("H", [4, 64])
+@pytest.mark.parametrize("new", [6, 20, 61])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+def test_unseen_rows_do_not_matter_in_tiles_with_idle_waves(kv, H, new, bad):
+    b = Batch([(150, new)], H=H, H_kv=2, kv=kv, seed=new)
+    b.queries.q_pos = b.put(b.pos)
+    clean, clean_lse = hisa.hisa_paged_attention(b.queries, b.cache, b.q_start, want_lse=True)
+    p = 150 + new // 2                                              # seen by the later half of the tokens
+    page, o = int(b.table[0, p // b.page]), p % b.page
+    for t, s in ((b.cache.k, b.cache.k_scale), (b.cache.v, b.cache.v_scale)):
+        if kv == "fp8":
+            s[page, o] = bad
+        else:
+            t[page, o, :, 1::3] = bad
+    out, lse = hisa.hisa_paged_attention(b.queries, b.cache, b.q_start, want_lse=True)
+    blind = new // 2
+    assert torch.equal(out[:blind], clean[:blind]) and torch.equal(lse[:blind], clean_lse[:blind])
+    assert not out[blind:].isfinite().all(dim=2).any()
+
+
+@pytest.mark.parametrize("d", [8, 64, 96, 128, 200, 256])
+@pytest.mark.parametrize("H,H_kv", [(40, 1), (70, 2), (3, 3)])
+def test_fp32_groups(d, H, H_kv):
+    b = Batch([(130, 3), (0, 40), (31, 1), (64, 0)], H=H, H_kv=H_kv, d=d, kv="f32", layout="apart", seed=d)
+    paged.run(b, what="fp32")
+    sparse.run(b, sparse.draw(b, 77, 1, holes=0.2), what="fp32")
