@@ -284,8 +284,9 @@ typedef struct {
  *               beyond max_pages * page)
  *   key_rows    [rows] out or NULL: q_seq * s_max + q_pos, the row of the token in a padded key array
  *               [n_seq, s_max, d] as hisa_keys describes it (-1: padding, or a position >= s_max)
- * Arrays must not overlap.  Limits: n_seq <= 65535, rows <= 4194304, n_seq * max_pages and max_pages *
- * page below 2^31, n_seq * s_max below 2^31 (with key_rows).  Needs no workspace.
+ * Positions stop at 2^31 - 1, a slot from 2^31 on is none.  Arrays must not overlap (seq_len == ctx_len,
+ * say, is refused).  Limits: n_seq <= 65535, rows <= 4194304, n_seq * max_pages and max_pages * page below
+ * 2^31, n_seq * s_max below 2^31 (with key_rows).  Needs no workspace.
  */
 int hisa_page_tables(const int32_t* ctx_len, const int32_t* new_len, int32_t n_seq, int32_t* block_table,
                      int32_t max_pages, int32_t page, const int32_t* free_pages, int32_t n_free, int32_t rows,

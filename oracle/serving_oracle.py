@@ -24,7 +24,7 @@ def page_tables(ctx_len, new_len, block_table, page, free_pages, rows, s_max=0):
         page_start.append(page_start[n] + need - had)
         q_start.append(min(rows, q_start[n] + new))
         for t in range(q_start[n], q_start[n + 1]):
-            pos = ctx + t - q_start[n]
+            pos = min(ctx + t - q_start[n], 2 ** 31 - 1)
             q_seq[t], q_pos[t] = n, pos
             if pos < end and table[n, pos // page] >= 0:
                 slots[t] = table[n, pos // page] * page + pos % page

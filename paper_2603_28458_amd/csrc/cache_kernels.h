@@ -116,13 +116,15 @@ __device__ __forceinline__ void table_row(const TableArgs& a, const Start& q_sta
   if (e < tokens) {
     seq = table_find(q_start, a.n_seq, e);
     const TableSeq s = table_seq(a, seq);
-    pos = s.ctx + e - (int)q_start[seq];
+    const long at_pos = (long)s.ctx + e - (int)q_start[seq];       // (a cached length may be any number)
+    pos = at_pos < 0x7fffffff ? (int)at_pos : 0x7fffffff;
     if (pos < s.len) {
       const int j = pos / a.page;
       // the page of a new entry is looked up where the entry comes from: its write is not waited for
       const int f = (int)page_start[seq] + j - s.had;
       const int id = j < s.had ? a.block_table[(long)seq * a.max_pages + j] : f < a.n_free ? a.free_pages[f] : -1;
-      if (id >= 0) slot = id * a.page + pos % a.page;
+      const long at = (long)id * a.page + pos % a.page;
+      if (id >= 0 && at < 1L << 31) slot = (int)at;
     }
     if (pos >= 0 && pos < a.s_max) key_row = seq * a.s_max + pos;
   }

@@ -264,6 +264,8 @@ int hisa_page_tables(const int32_t* ctx_len, const int32_t* new_len, int32_t n_s
     return HISA_ERR_SHAPE;
   if (overflows31(n_seq, max_pages) || overflows31(max_pages, page)) return HISA_ERR_SHAPE;
   if (key_rows && (s_max < 1 || overflows31(n_seq, s_max))) return HISA_ERR_SHAPE;
+  // (every workgroup reads the lengths that one of them would overwrite)
+  if (seq_len == ctx_len || seq_len == new_len) return HISA_ERR_SHAPE;
   TableArgs a{ctx_len, new_len, free_pages, block_table, seq_len, q_start,   page_start, q_seq, q_pos,
               slots,   key_rows, n_seq,     max_pages,   page,    n_free,    rows,       s_max};
   hipStream_t st = (hipStream_t)stream;

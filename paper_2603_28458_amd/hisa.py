@@ -560,6 +560,8 @@ def hisa_page_tables(ctx_len: torch.Tensor, new_len: torch.Tensor, block_table: 
     if block_table.dim() != 2 or block_table.shape[0] != n_seq:
         raise ValueError(f"block_table: shape {tuple(block_table.shape)}, needed is [{n_seq}, max_pages]")
     _fits(block_table, i32, block_table.shape, dev) or _need(block_table, "block_table", _I32, None, device)
+    if rows < 1:
+        raise ValueError(f"rows: {rows}")
     if out is None:
         out = PageTables.empty(n_seq, rows, device, key_rows=s_max > 0)
     st = _call(lib().hisa_page_tables, dev, stream, ctx_len.data_ptr(), new_len.data_ptr(), n_seq, block_table.data_ptr(),

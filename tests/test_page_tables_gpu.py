@@ -92,6 +92,19 @@ def test_negative_and_huge_lengths(n_seq):
     run(ctx, new, 8, 16, 500)
 
 
+@pytest.mark.parametrize("n_seq", [4, 1030])
+def test_positions_and_slots_past_31_bits(n_seq):
+    ctx, new = np.arange(n_seq) % 40, np.full(n_seq, 3)
+    ctx[1] = ctx[n_seq - 1] = 2 ** 31 - 2
+    run(ctx, new, 8, 16, 3 * n_seq + 5, s_max=100)
+    dev = torch.device("cuda:0")
+    put = lambda *a: torch.tensor(a, dtype=torch.int32, device=dev)  # noqa: E731
+    table = put([2 ** 27, -1], [7, -1])
+    t = hisa.hisa_page_tables(put(15, 3), put(2, 1), table, 16, put(2 ** 27 - 1), 4)
+    torch.cuda.synchronize()
+    assert t.slots.tolist() == [-1, (2 ** 27 - 1) * 16, 7 * 16 + 3, -1]
+
+
 def test_without_an_output_given():
     dev = torch.device("cuda:0")
     ctx, new = torch.tensor([5, 0], dtype=torch.int32, device=dev), torch.tensor([1, 3], dtype=torch.int32, device=dev)

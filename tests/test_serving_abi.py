@@ -122,7 +122,8 @@ def tables(lib, **kw):
     *[({n: None}, NULL) for n in ("ctx", "new", "table", "free", "seq_len", "q_start", "page_start", "q_seq", "q_pos", "slots")],
     (dict(n_seq=0), SHAPE), (dict(n_seq=65536), SHAPE), (dict(max_pages=0), SHAPE), (dict(page=0), SHAPE),
     (dict(n_free=-1), SHAPE), (dict(rows=0), SHAPE), (dict(rows=(1 << 22) + 1), SHAPE), (dict(max_pages=1 << 30), SHAPE),
-    (dict(page=1 << 28), SHAPE), (dict(key_rows=F), SHAPE), (dict(key_rows=F, s_max=1 << 30), SHAPE)])
+    (dict(page=1 << 28), SHAPE), (dict(key_rows=F), SHAPE), (dict(key_rows=F, s_max=1 << 30), SHAPE),
+    (dict(ctx=F + 64, new=F + 128, seq_len=F + 64), SHAPE), (dict(ctx=F + 64, new=F + 128, seq_len=F + 128), SHAPE)])
 def test_tables_refuse(lib, kw, status):  # noqa: F811
     assert tables(lib, **kw) == status
 
