@@ -53,8 +53,7 @@ __device__ __forceinline__ int last_seq(int n_seq, Le le) {
   return lo;
 }
 
-__device__ __forceinline__ int clamp_len(const AttnArgs& a, int n) {
-  const int len = a.seq_len[n];
+__device__ __forceinline__ int clamp_len(const AttnArgs& a, int len) {
   const long cap = (long)a.max_pages << a.page_shift;
   return len < 0 ? 0 : len < cap ? len : (int)cap;
 }
@@ -531,7 +530,7 @@ static __global__ __launch_bounds__(256, D > 128 ? 1 : 2) void k_attn_f32(AttnAr
     n = a.q_seq ? a.q_seq[t_begin] : 0;
     const bool none = (uint32_t)n >= (uint32_t)a.n_seq;
     n = none ? 0 : n;
-    len = none ? 0 : clamp_len(a, n);
+    len = none ? 0 : clamp_len(a, a.seq_len[n]);
     begin = 0;
     end = (a.n_list + 31) / 32;
   } else {
@@ -542,7 +541,7 @@ static __global__ __launch_bounds__(256, D > 128 ? 1 : 2) void k_attn_f32(AttnAr
     r0 = u.r0;
     rows = (t_end - t_begin) * a.G;
     if (r0 < 0 || r0 >= rows || t_begin < 0 || t_end > a.T) return;
-    len = clamp_len(a, n);
+    len = clamp_len(a, a.seq_len[n]);
   }
   int qr = r0 + col;
   const bool mine = qr < rows;
@@ -808,17 +807,26 @@ static __global__ __launch_bounds__(PAIR ? 512 : 256, 2) void k_attn_rows(AttnAr
     n = a.q_seq ? a.q_seq[t] : 0;
     const bool none = (uint32_t)n >= (uint32_t)a.n_seq;
     n = none ? 0 : n;
-    len = none ? 0 : clamp_len(a, n);
+    len = none ? 0 : clamp_len(a, a.seq_len[n]);
     begin = 0;
     end = (a.n_list + 31) / 32;
   } else {
-    n = last_seq(a.n_seq, [&](int i) { return a.q_start[i] <= t; });
-    const int t_end = a.q_start[n + 1];
-    if (t < a.q_start[n] || t >= t_end) return;
-    len = clamp_len(a, n);
-    const Seen s = seen_by(a, n, len, t, t_end);
-    lo = s.lo;
-    pos = s.pos;
+    // (one token per sequence is the common batch: everything about sequence t is asked for at once, and only if t is not
+    // its token is the right one searched: 200 sequences of 500 35.8 us, with a search first 36.6)
+    n = t < a.n_seq ? t : a.n_seq - 1;
+    int t_begin = a.q_start[n], t_end = a.q_start[n + 1], had = a.seq_len[n];
+    const int q_pos = a.q_pos ? a.q_pos[t] : 0, q_lo = a.q_lo ? a.q_lo[t] : 0;
+    if (t < t_begin || t >= t_end) {
+      n = last_seq(a.n_seq, [&](int i) { return a.q_start[i] <= t; });
+      t_begin = a.q_start[n];
+      t_end = a.q_start[n + 1];
+      if (t < t_begin || t >= t_end) return;
+      had = a.seq_len[n];
+    }
+    len = clamp_len(a, had);
+    pos = a.q_pos ? q_pos : had - t_end + t;
+    pos = pos < len ? pos : len - 1;
+    lo = q_lo > 0 ? q_lo : 0;
     begin = lo >> 5;
     end = (pos + 32) >> 5;
     if (pos < 0 || end < begin) end = begin;
@@ -1066,10 +1074,20 @@ static __global__ __launch_bounds__(512, 2) void k_attn_chunk(AttnArgs a) {
   const int n = u.n, t_begin = u.t_begin, t_end = u.t_end;
   const int r0 = u.r0, rows = (t_end - t_begin) * a.G;
   if (r0 < 0 || r0 >= rows || t_begin < 0 || t_end > a.T) return;
-  const int len = clamp_len(a, n);
+  const int len = clamp_len(a, a.seq_len[n]);
   const int32_t* __restrict__ table = a.table + (long)n * a.max_pages;
 
-  // what the whole tile of rows sees, and what this wave's rows see
+  // what this wave's rows see, and what the whole tile of rows sees
+  RowState<D> st[1];
+  int qr = r0 + wave * 32 + col;
+  const bool mine = qr < rows;
+  if (!mine) qr = rows - 1;
+  const int t = t_begin + qr / a.G, h = hk * a.G + qr % a.G;
+  {
+    const Seen s = seen_by(a, n, len, t, t_end);
+    st[0].pos = s.pos;
+    st[0].lo = s.lo;
+  }
   int wg_pos = -1, wg_lo = 0x7fffffff, wg_pos_min = 0x7fffffff, wg_lo_max = 0;
   {
     const int last = r0 + kChunkRows - 1 < rows - 1 ? r0 + kChunkRows - 1 : rows - 1;
@@ -1080,23 +1098,13 @@ static __global__ __launch_bounds__(512, 2) void k_attn_chunk(AttnArgs a) {
       wg_pos_min = s.pos < wg_pos_min ? s.pos : wg_pos_min;
       wg_lo_max = s.lo > wg_lo_max ? s.lo : wg_lo_max;
     }
-    wg_pos_min = wave_min_int(wg_pos_min);
-    wg_lo_max = wave_max_int(wg_lo_max);
-    wg_pos = wave_max_int(wg_pos);
-    wg_lo = wave_min_int(wg_lo);
   }
-  RowState<D> st[1];
-  int qr = r0 + wave * 32 + col;
-  const bool mine = qr < rows;
-  if (!mine) qr = rows - 1;
-  const int t = t_begin + qr / a.G, h = hk * a.G + qr % a.G;
   st[0].clear();
   st[0].load_q((const uint16_t*)a.q + ((long)t * a.H + h) * D);
-  {
-    const Seen s = seen_by(a, n, len, t, t_end);
-    st[0].pos = s.pos;
-    st[0].lo = s.lo;
-  }
+  wg_pos_min = wave_min_int(wg_pos_min);
+  wg_lo_max = wave_max_int(wg_lo_max);
+  wg_pos = wave_max_int(wg_pos);
+  wg_lo = wave_min_int(wg_lo);
   const int pos_min = wave_min_int(st[0].pos), lo_max = wave_max_int(st[0].lo);
 
   int begin = wg_lo / kChunkKeys, end = (wg_pos + kChunkKeys) / kChunkKeys;
