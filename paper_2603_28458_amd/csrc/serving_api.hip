@@ -4,6 +4,7 @@
 
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cmath>
 
 #include "api_common.h"
@@ -67,6 +68,24 @@ struct AttnPlan {
 
 constexpr long kCus = 256, kPartKeys = 256;
 
+// Parts of the keys of `units` workgroups, of which `fit` run at a time, by the time until the last one is done.  A part
+// costs as much as 512 keys beside its own (lists and ranges of 44 shapes, geometric mean: 128 38.0 us, 256 36.3, 512 35.5,
+// 768 35.6, 1024 35.6; always filling the machine once 39.3).  uneven: sequences of a batch differ in length, which several
+// rounds even out.
+long parts(long units, long fit, long keys, long most, bool uneven) {
+  long best = 0, last = 0;
+  double least = 0;
+  for (int j = 1; j <= 16; ++j) {            // (as many as j rounds hold)
+    const long s = std::max(1L, std::min(most, j * fit / units));
+    if (s == last) continue;
+    last = s;
+    const double rounds = (double)units * s / fit, one = (double)keys / s + 512;
+    const double time = one * (rounds <= 1 ? 1. : uneven ? 0.88 * rounds + 0.4 : std::ceil(rounds));
+    if (!best || time < least) least = time, best = s;
+  }
+  return best;
+}
+
 AttnPlan plan_attention(const hisa_queries* q, const hisa_cache* c, int32_t k) {
   AttnPlan p{};
   const long keys = k ? k : (long)c->max_pages * c->page;
@@ -86,9 +105,8 @@ AttnPlan plan_attention(const hisa_queries* q, const hisa_cache* c, int32_t k) {
   if (c->dtype == HISA_F32) {
     p.kernel = ATTN_F32;
     p.units = k ? T * ((G + 31) / 32) : T * G / 32 + c->n_seq;
-    const long wgs = p.units * c->H_kv;
     most = (keys + 127) / 128;
-    splits = wgs < 2 * kCus ? 2 * kCus / wgs : 1;          // two workgroups per CU
+    splits = parts(p.units * c->H_kv, (c->d > 128 ? 1 : 2) * kCus, keys, most, !k);
   } else if (k || T <= few * c->n_seq) {
     p.kernel = ATTN_ROWS;
     // (one gathering of the keys for up to 64 heads: lists of 2048, 64 heads on one KV head, 1024 queries 155 us, two
@@ -96,27 +114,13 @@ AttnPlan plan_attention(const hisa_queries* q, const hisa_cache* c, int32_t k) {
     p.pair = G > 32;
     const long heads = p.pair ? 64 : 32;
     p.units = T * ((G + heads - 1) / heads);
-    // Two workgroups fit a CU, one with PAIR.  Over ranges four rounds of them even out sequences of different lengths (200
-    // sequences, 4 KV heads, fp8: 2 parts 468 us, 3 parts 490); lists are alike, and every part more is one more to join (100
-    // lists of 2048: 5 parts 41 us, 6 parts 48).
-    const long wgs = p.units * c->H_kv, want = k ? 2 * kCus : 8 * kCus;
-    splits = wgs < want ? want / wgs : 1;
+    splits = parts(p.units * c->H_kv, (p.pair ? 1 : 2) * kCus, keys, most, !k);
   } else {
     p.kernel = ATTN_CHUNK;
     p.units = T * G / kChunkRows + c->n_seq;
-    // One workgroup per CU: the parts with which the last one is done first, if all sequences were alike; a part costs as
-    // much as 512 keys before and after its tiles.  (10 sequences of 5000, 30 new tokens each: 3 parts 75 us, 2 parts 91;
-    // one of 3000 with 700: 4 parts 110 us, 2 parts 137.)
-    const long each = (T * G + (long)c->n_seq * kChunkRows - 1) / ((long)c->n_seq * kChunkRows);
-    const long busy = each * c->n_seq * c->H_kv;
-    long best = 0;
-    splits = 1;
-    for (long s = 1; s <= most && (s == 1 || busy * s <= 4 * kCus); ++s) {
-      const long cost = (busy * s + kCus - 1) / kCus * ((keys + s - 1) / s + 512);
-      if (s == 1 || cost < best) best = cost, splits = s;
-    }
+    const long each = (T * G + (long)c->n_seq * kChunkRows - 1) / ((long)c->n_seq * kChunkRows);   // (if all were alike)
+    splits = parts(each * c->n_seq * c->H_kv, kCus, keys, most, false);
   }
-  if (splits > most) splits = most;
   p.splits = (int)splits;
   p.ws_bytes = splits > 1 ? (size_t)splits * T * q->H * (c->d + 2) * 4 : 0;
   return p;
