@@ -310,11 +310,10 @@ int hisa_cache_append(const hisa_cache* cache, const int32_t* slots, const void*
   a.R = cache->H_kv;
   a.d = cache->d;
   a.page = cache->page;
-  a.arrays = v_new ? 2 : 1;
   a.lanes = 1;
   while (a.lanes * 8 < a.d) a.lanes *= 2;
   a.n_slots = (long)cache->n_pages * cache->page;
-  const long rows = (long)T * a.R * a.arrays, per = 256 / a.lanes, wgs = (rows + per - 1) / per;
+  const long rows = (long)T * a.R, per = 256 / a.lanes, wgs = (rows + per - 1) / per;
   if (wgs > kMaxGrid) return HISA_ERR_SHAPE;
   if (src_dtype == HISA_F32) launch_append<0>(a, cache->dtype, dim3((unsigned)wgs), (hipStream_t)stream);
   else launch_append<1>(a, cache->dtype, dim3((unsigned)wgs), (hipStream_t)stream);
