@@ -304,7 +304,8 @@ int hisa_page_tables(const int32_t* ctx_len, const int32_t* new_len, int32_t n_s
  * which part of each) is unspecified.  The indexer's padded key array is a cache of n_seq pages of
  * s_max rows with one head and no values, and hisa_page_tables gives its slots as key_rows.
  * block_table and seq_len are not read (may be NULL).  d % 8 == 0, d <= 512, strides multiples of 8;
- * n_pages * page below 2^31; k, v, k_new, v_new 16-byte aligned, src_stride a multiple of 8.
+ * n_pages * page below 2^31; k, v, k_new, v_new 16-byte aligned, src_stride a multiple of 8; T * H_kv *
+ * d (rounded up to a power of two) below 2^35.
  * Needs no workspace.
  */
 int hisa_cache_append(const hisa_cache* cache, const int32_t* slots, const void* k_new, const void* v_new,
@@ -329,7 +330,8 @@ int hisa_cache_append(const hisa_cache* cache, const int32_t* slots, const void*
  * Supported: q BF16 with a BF16 or FP8_E4M3 cache, d in {64, 128}; q F32 with an F32 cache, d % 4 == 0,
  * d <= 256.  H <= 256, H_kv divides H; page a power of two; k, v and q 16-byte aligned, strides times
  * the element size multiples of 16 bytes; max_pages * page and n_pages * page below 2^31;
- * scale positive and finite.
+ * scale positive and finite.  A launch holds fewer than 2^23 workgroups: split larger calls.  What always
+ * fits: T * H_kv * ceil(H / H_kv / 32) below that (lists), T * H / 32 + 4 * n_seq * H_kv (ranges).
  * Scores, the running maximum and sum and the output are held in fp32; for the second product (bf16 and
  * fp8 caches) the weights p_s are rounded to bf16, where T * H <= 1024 to two bf16 parts (16 bits).  All
  * sums have a fixed order: the same call gives the same bits.

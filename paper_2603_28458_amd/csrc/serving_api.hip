@@ -17,6 +17,8 @@ namespace {
 
 constexpr int kMaxHeads = 256, kMaxList = 65536, kMaxAppendD = 512;
 
+constexpr long kMaxThreads = (1L << 32) - 1;   // of a launch: the packet counts them in 32 bits
+
 inline int elem_bytes(int dtype) { return dtype == HISA_F32 ? 4 : dtype == HISA_BF16 ? 2 : 1; }
 inline bool overflows31(long a, long b) { return a * b >= (1L << 31); }   // (both below 2^31)
 
@@ -195,7 +197,7 @@ int launch_f32(const AttnArgs& a, dim3 grid, hipStream_t st) {
 template <bool LIST>
 int launch_attention(AttnArgs a, const AttnPlan& p, int dtype, hipStream_t st) {
   const long wgs = p.units * a.H_kv * a.splits;
-  if (wgs > kMaxGrid) return HISA_ERR_SHAPE;
+  if (wgs * 512 > kMaxThreads) return HISA_ERR_SHAPE;
   const dim3 grid((unsigned)wgs);
   int status = HISA_OK;
   if (dtype == HISA_F32)
@@ -314,7 +316,7 @@ int hisa_cache_append(const hisa_cache* cache, const int32_t* slots, const void*
   while (a.lanes * 8 < a.d) a.lanes *= 2;
   a.n_slots = (long)cache->n_pages * cache->page;
   const long rows = (long)T * a.R, per = 256 / a.lanes, wgs = (rows + per - 1) / per;
-  if (wgs > kMaxGrid) return HISA_ERR_SHAPE;
+  if (wgs * 256 > kMaxThreads) return HISA_ERR_SHAPE;
   if (src_dtype == HISA_F32) launch_append<0>(a, cache->dtype, dim3((unsigned)wgs), (hipStream_t)stream);
   else launch_append<1>(a, cache->dtype, dim3((unsigned)wgs), (hipStream_t)stream);
   return launch_status();

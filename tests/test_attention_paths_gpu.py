@@ -99,3 +99,28 @@ def test_fp32_groups(d, H, H_kv):
     b = Batch([(130, 3), (0, 40), (31, 1), (64, 0)], H=H, H_kv=H_kv, d=d, kv="f32", layout="apart", seed=d)
     paged.run(b, what="fp32")
     sparse.run(b, sparse.draw(b, 77, 1, holes=0.2), what="fp32")
+
+
+@pytest.mark.parametrize("kv,d", [("bf16", 128), ("fp8", 64), ("f32", 36), ("f32", 128)])
+@pytest.mark.parametrize("lens,H,H_kv", [([(3000, 1), (70, 1)], 8, 2), ([(700, 33), (0, 5), (9, 0)], 14, 2), ([(5000, 1)], 100, 1),
+                                         ([(60, 300)], 4, 1)])
+def test_nothing_beside_the_outputs_and_the_workspace_is_written(kv, d, lens, H, H_kv):
+    b = Batch(lens, H=H, H_kv=H_kv, d=d, kv=kv, page=64, seed=d)
+    b.queries.q_pos = b.put(b.pos)
+    lists = b.put(sparse.draw(b, 600, 3))
+    for k in (0, 600):
+        size = hisa.hisa_attention_workspace_bytes(b.queries, b.cache, k)
+        sizes = (b.T * H * d * b.queries.q.element_size(), b.T * H * 4, max(size, 16))
+        bufs = [torch.full((n + 2048,), 0xA5, dtype=torch.uint8, device=b.dev) for n in sizes]
+        out, lse, ws = (x[1024:1024 + n] for x, n in zip(bufs, sizes))
+        out, lse = out.view(b.queries.q.dtype).view(b.T, H, d), lse.view(torch.float32).view(b.T, H)
+        if k:
+            hisa.hisa_sparse_attention(b.queries, b.cache, lists, out=out, lse=lse, ws=ws)
+        else:
+            hisa.hisa_paged_attention(b.queries, b.cache, b.q_start, out=out, lse=lse, ws=ws)
+        torch.cuda.synchronize()
+        for x in bufs:
+            assert (x[:1024] == 0xA5).all() and (x[-1024:] == 0xA5).all()
+        want = (hisa.hisa_sparse_attention(b.queries, b.cache, lists) if k
+                else hisa.hisa_paged_attention(b.queries, b.cache, b.q_start))[0]
+        assert torch.equal(out, want)

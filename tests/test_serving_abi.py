@@ -89,6 +89,13 @@ def test_attention_refuses_the_rest(lib):  # noqa: F811
         assert paged(lib, queries(q_dtype=F32), cache(dtype=F32, d=d)) == status
 
 
+def test_launches_beyond_32_bits_of_threads_are_refused(lib):  # noqa: F811
+    many = queries(T=1 << 22, H=64)
+    assert sparse(lib, many, cache(H_kv=8, head_stride=128, token_stride=1024), k=1) == SHAPE
+    assert paged(lib, queries(T=131070, H=256), cache(H_kv=256, n_seq=65535, token_stride=256 * 128, max_pages=1)) == SHAPE
+    assert append(lib, cache(H_kv=64, d=512, token_stride=64 * 512, head_stride=512), stride=64 * 512, T=1 << 22) == SHAPE
+
+
 def append(lib, c, slots=F, k=F, v=F, dt=BF16, stride=256, T=4):
     return lib.hisa_cache_append(C.byref(c) if c else None, slots, k, v, dt, stride, T, None)
 
