@@ -494,6 +494,7 @@ __device__ __forceinline__ void store_result(const AttnArgs& a, int split, long 
 // values take their registers, and the next keys theirs: each is under way for as long as the other is multiplied.  The scores' accumulator holds keys
 // 8 j + 4 half + x in register 4 j + x, so product 4 j + x of the values takes those two keys and that register as it is.
 // Bound by memory where a KV head's group is small (8 D bytes per key), by the fp32 matrix units where 32 rows are real.
+// Measured, d = 128, 64 heads on 8: 32 tokens over 16384 keys each 0.80 ms, 4.7 TB/s; 800 over 3000 0.66 ms, 94 TFLOP/s.
 constexpr int kF32MaxD = 256;
 
 template <int D>
@@ -765,7 +766,9 @@ static __global__ __launch_bounds__(256, D > 128 ? 1 : 2) void k_attn_f32(AttnAr
 // second one beside it on its SIMD: one brings the keys of their tile, the other the values, and each multiplies 32 of the
 // heads, so that wider groups gather every row once and still leave each SIMD two waves.  All rows see the same keys, so a
 // row outside is a row of zeros and a score of -inf for everybody.  Bound by memory: 4 D bytes (bf16) per key and KV head,
-// whatever the number of heads.
+// whatever the number of heads.  Measured, d = 128: one token of 32 sequences of up to 131072, 64 heads on 8 KV heads, 2.54
+// ms, 5.9 TB/s; of 200 short ones, 4 KV heads, fp8, 0.47 ms, 4.8 TB/s (a workgroup there is a quarter start and end); 1024
+// lists of 2048, 64 heads on one KV head, 136 us (8 TB/s gathered, from L2 for the most part).
 constexpr int kRowWaves = 4;
 
 template <int D, int KDT, bool PAIR>
@@ -1017,7 +1020,9 @@ static __global__ __launch_bounds__(PAIR ? 512 : 256, 2) void k_attn_rows(AttnAr
 
 // ---- many rows per sequence ----------------------------------------------------------------------
 // A workgroup of 8 waves takes 256 query rows of one KV head (32 per wave) and a part of their keys, in tiles of 64 keys
-// that all waves multiply from LDS.  Bound by the matrix units (4 D flop per visible pair).  Each SIMD holds two waves, one
+// that all waves multiply from LDS.  Bound by the matrix units (4 D flop per visible pair) and, for d = 64, by the vector
+// units that make the weights.  Measured: 1024 tokens behind 64K, 64 heads on 8, d = 128, 2.05 ms, 1.06 PFLOP/s (fp8 2.3 ms);
+// eleven prompts of 2777 tokens at most, windows of 1024, 32 heads on 2, d = 64, fp8, 0.53 ms, 0.42.  Each SIMD holds two waves, one
 // of the first four (group 0) and one of the last four (group 1).  In interval i, between two barriers, group 0 turns its
 // scores of tile i into weights, then runs its products for tile i + 1 (scores of tile i + 1, values of tile i), while
 // group 1 runs its products for tile i, then turns those scores into weights: one computes while the other multiplies, and
@@ -1377,7 +1382,8 @@ static __global__ __launch_bounds__(512, 2) void k_attn_chunk(AttnArgs a) {
 }
 
 // Joins the parts of a row: 4 columns per lane, 8 parts asked for at once (what this costs is the way to memory, once per
-// 8 parts), `groups` sets of lanes per row that share its parts and meet in LDS.
+// 8 parts), `groups` sets of lanes per row that share its parts and meet in LDS.  (One token over 130000 keys, 64 heads on
+// one KV head, 128 parts: with one set per row and a part at a time the call took 341 us, so 42.)
 constexpr int kJoinParts = 8;
 
 struct Joined {
