@@ -129,7 +129,6 @@ __device__ __forceinline__ int renewed(int x) {
 }
 
 // 16 stored bytes of a row as they go into a tile: bf16 as they are, fp8 widened (exactly) into two chunks.
-template <int KDT>
 __device__ __forceinline__ uint4 widen_fp8(uint32_t lo, uint32_t hi) {
   const uint2 a = fp8x4_to_bf16x4(lo), b = fp8x4_to_bf16x4(hi);
   return make_uint4(a.x, a.y, b.x, b.y);
@@ -138,7 +137,7 @@ template <int D, int KDT, bool VALUES>
 __device__ __forceinline__ void store_chunk(unsigned char* tile, int r, int c, uint4 x) {
   using R = RowTile<D>;
   if constexpr (KDT == 2) {
-    const uint4 a = widen_fp8<KDT>(x.x, x.y), b = widen_fp8<KDT>(x.z, x.w);
+    const uint4 a = widen_fp8(x.x, x.y), b = widen_fp8(x.z, x.w);
     *reinterpret_cast<uint4*>(tile + (VALUES ? R::value_byte(r, 2 * c) : R::key_byte(r, 2 * c))) = a;
     *reinterpret_cast<uint4*>(tile + (VALUES ? R::value_byte(r, 2 * c + 1) : R::key_byte(r, 2 * c + 1))) = b;
   } else {
@@ -355,20 +354,15 @@ __device__ __forceinline__ void add_odd_values(RowState<D>& st, const unsigned c
   }
 }
 
-template <int D, int NB, int NQ>
-__device__ __forceinline__ void score_tile(const RowState<D> (&st)[NQ], const unsigned char* tile, int read_key, f32x16 (&s)[NQ][NB]) {
+template <int D, int NB>
+__device__ __forceinline__ void score_tile(const RowState<D>& st, const unsigned char* tile, int read_key, f32x16 (&s)[NB]) {
 #pragma unroll
   for (int b = 0; b < NB; ++b) {
 #pragma unroll
-    for (int n = 0; n < NQ; ++n)
+    for (int i = 0; i < 16; ++i) s[b][i] = 0.f;
 #pragma unroll
-      for (int i = 0; i < 16; ++i) s[n][b][i] = 0.f;
-#pragma unroll
-    for (int kk = 0; kk < D / 16; ++kk) {
-      const bf16x8 a = RowTile<D>::key_operand(tile, read_key, 32 * b, kk);
-#pragma unroll
-      for (int n = 0; n < NQ; ++n) s[n][b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, st[n].q[kk], s[n][b], 0, 0, 0);
-    }
+    for (int kk = 0; kk < D / 16; ++kk)
+      s[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(RowTile<D>::key_operand(tile, read_key, 32 * b, kk), st.q[kk], s[b], 0, 0, 0);
   }
 }
 
@@ -491,8 +485,9 @@ __device__ __forceinline__ void store_result(const AttnArgs& a, int split, long 
 // works alone on every fourth tile of 32 keys, and the waves' results are joined at the end.  Operands come straight from
 // memory: of a key row lane half h reads elements 8 kk + 4 h + 0..3 and spends them on four products (a contraction may
 // take its index in any order), a value row is read 32 columns at a time by 32 lanes.  As the keys of a tile are used up the
-// values take their registers, and the next keys theirs: each is under way for as long as the other is multiplied.  The scores' accumulator holds keys
-// 8 j + 4 half + x in register 4 j + x, so product 4 j + x of the values takes those two keys and that register as it is.
+// values take their registers, and the next keys theirs: each is under way for as long as the other is multiplied.  The
+// scores' accumulator holds keys 8 j + 4 half + x in register 4 j + x, so product 4 j + x of the values takes those two keys
+// and that register as it is.
 // Bound by memory where a KV head's group is small (8 D bytes per key), by the fp32 matrix units where 32 rows are real.
 // Measured, d = 128, 64 heads on 8: 32 tokens over 16384 keys each 0.80 ms, 4.7 TB/s; 800 over 3000 0.66 ms, 94 TFLOP/s.
 constexpr int kF32MaxD = 256;
@@ -915,7 +910,7 @@ static __global__ __launch_bounds__(PAIR ? 512 : 256, 2) void k_attn_rows(AttnAr
 
   // page lookups run one tile ahead of the rows, list entries two
   int tile = begin + lead, s_next, p_next, s_after;
-  RowState<D> st[1];
+  RowState<D> st;
   {
     constexpr int kD = Geo::kDepth;
     int s[kD + 2], p[kD + 1];
@@ -929,8 +924,8 @@ static __global__ __launch_bounds__(PAIR ? 512 : 256, 2) void k_attn_rows(AttnAr
     s_after = s[kD + 1];
     int r = r0 + col;                           // (columns beyond the last head repeat it and are not stored)
     if (r >= a.G) r = a.G - 1;
-    st[0].clear();
-    st[0].load_q((const uint16_t*)a.q + ((long)t * a.H + hk * a.G + r) * D);
+    st.clear();
+    st.load_q((const uint16_t*)a.q + ((long)t * a.H + hk * a.G + r) * D);
   }
   const int read_key = RowTile<D>::read_key(), read_value = RowTile<D>::read_value();
   int turn = 0;
@@ -948,16 +943,16 @@ static __global__ __launch_bounds__(PAIR ? 512 : 256, 2) void k_attn_rows(AttnAr
     p_next = page_of(s_next);
     s_after = position(tile + (Geo::kDepth + 2) * kRowWaves);
     if (!PAIR || tile < end) {
-      f32x16 s[1][1];
-      bf16x8 p[1][2], rest[1][2];
-      score_tile<D, 1, 1>(st, kt, renewed(read_key), s);
-      if constexpr (KDT == 2) scale_scores<1>(s[0], sc);
+      f32x16 s[1];
+      bf16x8 p[2], rest[2];
+      score_tile<D, 1>(st, kt, renewed(read_key), s);
+      if constexpr (KDT == 2) scale_scores<1>(s, sc);
       if (keys != 0xffffffffu) {
         asm volatile("");                       // (a branch, not selects for every tile)
-        hide_keys(s[0][0], keys);
+        hide_keys(s[0], keys);
       }
-      softmax_tile<D, KDT, 1, REST>(st[0], s[0], p[0], rest[0], a.scale_log2, sc + 32);
-      add_values<D, REST>(st[0], vt, renewed(read_value), p[0], rest[0]);
+      softmax_tile<D, KDT, 1, REST>(st, s, p, rest, a.scale_log2, sc + 32);
+      add_values<D, REST>(st, vt, renewed(read_value), p, rest);
     }
     if constexpr (!PAIR) wave_lds_order();
     tile += kRowWaves;
@@ -974,9 +969,9 @@ static __global__ __launch_bounds__(PAIR ? 512 : 256, 2) void k_attn_rows(AttnAr
 
   // the waves' shares of every row, joined
   float* part = reinterpret_cast<float*>(lds);                  // [wave][D][32]
-  const float l = add_halves(st[0].l);
+  const float l = add_halves(st.l);
   if (half == 0) {
-    join[(wave * 32 + col) * 2] = st[0].m;
+    join[(wave * 32 + col) * 2] = st.m;
     join[(wave * 32 + col) * 2 + 1] = l;
   }
   __syncthreads();
@@ -991,12 +986,12 @@ static __global__ __launch_bounds__(PAIR ? 512 : 256, 2) void k_attn_rows(AttnAr
     const float* ml = join + ((first + w) * 32 + col) * 2;
     sum = __builtin_fmaf(__builtin_amdgcn_exp2f(ml[0] - base), ml[1], sum);
   }
-  const float f = __builtin_amdgcn_exp2f(st[0].m - base);
+  const float f = __builtin_amdgcn_exp2f(st.m - base);
 #pragma unroll
   for (int dt = 0; dt < D / 32; ++dt)
 #pragma unroll
     for (int i = 0; i < 16; ++i)
-      part[(wave * D + dt * 32 + 8 * (i >> 2) + 4 * half + (i & 3)) * 32 + col] = st[0].o[dt][i] * f;
+      part[(wave * D + dt * 32 + 8 * (i >> 2) + 4 * half + (i & 3)) * 32 + col] = st.o[dt][i] * f;
   __syncthreads();
   const int r = r0 + col;
   if (r < a.G) {
@@ -1054,10 +1049,12 @@ struct ChunkGeom {
 
 // 16 or 4 bytes per lane from `src` to LDS byte lds + 16 (or 4) * lane.  (Nothing else here has a use for m0.)
 __device__ __forceinline__ void dma16(uint32_t lds, const void* src) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(__builtin_amdgcn_readfirstlane((int)lds)), "v"(src) : "memory");
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::
+               "s"(__builtin_amdgcn_readfirstlane((int)lds)), "v"(src) : "memory");
 }
 __device__ __forceinline__ void dma4(uint32_t lds, const void* src) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(__builtin_amdgcn_readfirstlane((int)lds)), "v"(src) : "memory");
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::
+               "s"(__builtin_amdgcn_readfirstlane((int)lds)), "v"(src) : "memory");
 }
 template <int N>
 __device__ __forceinline__ void dma_left() {   // until at most N requests of this wave are under way
@@ -1083,15 +1080,15 @@ static __global__ __launch_bounds__(512, 2) void k_attn_chunk(AttnArgs a) {
   const int32_t* __restrict__ table = a.table + (long)n * a.max_pages;
 
   // what this wave's rows see, and what the whole tile of rows sees
-  RowState<D> st[1];
+  RowState<D> st;
   int qr = r0 + wave * 32 + col;
   const bool mine = qr < rows;
   if (!mine) qr = rows - 1;
   const int t = t_begin + qr / a.G, h = hk * a.G + qr % a.G;
   {
     const Seen s = seen_by(a, n, len, t, t_end);
-    st[0].pos = s.pos;
-    st[0].lo = s.lo;
+    st.pos = s.pos;
+    st.lo = s.lo;
   }
   int wg_pos = -1, wg_lo = 0x7fffffff, wg_pos_min = 0x7fffffff, wg_lo_max = 0;
   {
@@ -1104,13 +1101,13 @@ static __global__ __launch_bounds__(512, 2) void k_attn_chunk(AttnArgs a) {
       wg_lo_max = s.lo > wg_lo_max ? s.lo : wg_lo_max;
     }
   }
-  st[0].clear();
-  st[0].load_q((const uint16_t*)a.q + ((long)t * a.H + h) * D);
+  st.clear();
+  st.load_q((const uint16_t*)a.q + ((long)t * a.H + h) * D);
   wg_pos_min = wave_min_int(wg_pos_min);
   wg_lo_max = wave_max_int(wg_lo_max);
   wg_pos = wave_max_int(wg_pos);
   wg_lo = wave_min_int(wg_lo);
-  const int pos_min = wave_min_int(st[0].pos), lo_max = wave_max_int(st[0].lo);
+  const int pos_min = wave_min_int(st.pos), lo_max = wave_max_int(st.lo);
 
   int begin = wg_lo / kChunkKeys, end = (wg_pos + kChunkKeys) / kChunkKeys;
   if (wg_pos < 0 || end < begin) end = begin;
@@ -1293,10 +1290,10 @@ static __global__ __launch_bounds__(512, 2) void k_attn_chunk(AttnArgs a) {
     dma_left<0>();
     return;
   }
-  f32x16 s[1][2];
-  bf16x8 p[1][4], rest[4];
+  f32x16 s[2];
+  bf16x8 p[4], rest[4];
   if (group == 1) lds_barrier();
-  score_tile<D, 2, 1>(st, lds + key_tile(r), renewed(read_key), s);
+  score_tile<D, 2>(st, lds + key_tile(r), renewed(read_key), s);
   {
     // (fp8: what group 1 widens here, and group 0 between the products for the next tile, came with the third request)
     const int tile = begin + group;
@@ -1311,21 +1308,21 @@ static __global__ __launch_bounds__(512, 2) void k_attn_chunk(AttnArgs a) {
     const uint64_t mask = mask_of(tile), km = mask_of(tile + 2), vm = mask_of(tile + 1);
     {
       const float* sc = scales + (tile & 7) * 2 * kChunkKeys;
-      if constexpr (KDT == 2) scale_scores<2>(s[0], sc);
+      if constexpr (KDT == 2) scale_scores<2>(s, sc);
       if (mask != ~0ull || base + kChunkKeys - 1 > pos_min || base < lo_max) {
         asm volatile("");                  // (a branch, not 32 selects for every tile)
-        hide(st[0], s[0][0], (uint32_t)mask, base);
-        hide(st[0], s[0][1], (uint32_t)(mask >> 32), base + 32);
+        hide(st, s[0], (uint32_t)mask, base);
+        hide(st, s[1], (uint32_t)(mask >> 32), base + 32);
       }
-      softmax_tile<D, KDT, 2, REST>(st[0], s[0], p[0], rest, a.scale_log2, sc + kChunkKeys);
+      softmax_tile<D, KDT, 2, REST>(st, s, p, rest, a.scale_log2, sc + kChunkKeys);
     }
     // (the weights are made here and not, as the compiler would have it, between the products that need them)
 #pragma unroll
-    for (int i = 0; i < 4; ++i) asm volatile("" : "+v"(p[0][i]));
+    for (int i = 0; i < 4; ++i) asm volatile("" : "+v"(p[i]));
     if constexpr (REST)
 #pragma unroll
       for (int i = 0; i < 4; ++i) asm volatile("" : "+v"(rest[i]));
-    asm volatile("" : "+v"(st[0].l));
+    asm volatile("" : "+v"(st.l));
     if (wave == 0) publish(tile + 5, pages[((tile + 5) & 7) * kChunkKeys + lane]);
     if (group == 1) {
       if constexpr (KDT == 1) {
@@ -1347,14 +1344,15 @@ static __global__ __launch_bounds__(512, 2) void k_attn_chunk(AttnArgs a) {
     Where at;
     constexpr int kProducts = D / 4;
     __builtin_amdgcn_s_setprio(3);           // (the wave that multiplies goes first: 0.5 % at 1024 new tokens behind 64K)
-    products<D, REST>(st[0], lds + key_tile(r1), renewed(read_key), s[0], lds + value_tile(r), renewed(read_value), p[0], rest, [&](int i) {
+    products<D, REST>(st, lds + key_tile(r1), renewed(read_key), s, lds + value_tile(r), renewed(read_value), p, rest,
+                      [&](int i) {
       if (i == 1) at = where(asked);
       // (fp8: the buffer of the step before the one that is widened now)
       if (i == kProducts / 4) request(asked, at, KDT == 2 ? (group == 0 ? r1 : r2) : asked & 3, tile + 7 + (KDT == 2));
     });
     __builtin_amdgcn_s_setprio(0);
     if (dropped)
-      add_odd_values<D, KDT>(st[0], (const unsigned char*)a.v + hk * a.head_stride * kBytes, offsets + (tile & 7) * kChunkKeys,
+      add_odd_values<D, KDT>(st, (const unsigned char*)a.v + hk * a.head_stride * kBytes, offsets + (tile & 7) * kChunkKeys,
                              slots + (tile & 7) * kChunkKeys, a.v_scale + hk, a.H_kv, base);
     if (group == 0) {
       if constexpr (KDT == 1) {
@@ -1368,16 +1366,16 @@ static __global__ __launch_bounds__(512, 2) void k_attn_chunk(AttnArgs a) {
   dma_left<0>();                           // (LDS is somebody else's once the workgroup has ended)
 
   if (!mine) return;
-  const float l = add_halves(st[0].l);
+  const float l = add_halves(st.l);
   const long row = (long)t * a.H + h;
 #pragma unroll
   for (int dt = 0; dt < D / 32; ++dt)
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       const int e = dt * 32 + 8 * j + 4 * half;
-      const float4 o = make_float4(st[0].o[dt][4 * j], st[0].o[dt][4 * j + 1], st[0].o[dt][4 * j + 2], st[0].o[dt][4 * j + 3]);
-      if (a.splits > 1) store_result<1, true>(a, split, row, D, e, o, st[0].m, l);
-      else store_result<1, false>(a, split, row, D, e, o, st[0].m, l);
+      const float4 o = make_float4(st.o[dt][4 * j], st.o[dt][4 * j + 1], st.o[dt][4 * j + 2], st.o[dt][4 * j + 3]);
+      if (a.splits > 1) store_result<1, true>(a, split, row, D, e, o, st.m, l);
+      else store_result<1, false>(a, split, row, D, e, o, st.m, l);
     }
 }
 

@@ -6,6 +6,7 @@ library is missing, the first call raises.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes as C
 import os
 from dataclasses import dataclass
@@ -431,6 +432,17 @@ def _call(fn, dev: int, stream, *args) -> int:
         return fn(*args, _stream(stream))
 
 
+def _allocating(stream, device):
+    """Where a call allocates what it was not given: on the stream that it runs on, so that the memory is not handed out
+    again before the kernels are done with it."""
+    if stream is None:
+        return contextlib.nullcontext()
+    if not isinstance(stream, torch.cuda.Stream):
+        handle = _stream(stream)
+        stream = torch.cuda.ExternalStream(handle, device=device) if handle else torch.cuda.default_stream(device)
+    return torch.cuda.stream(stream)
+
+
 @dataclass
 class Cache:
     """A paged cache: k, v [n_pages, page, H_kv, d] (float32 / bfloat16 / uint8 or float8 codes; any strides that k and v
@@ -563,7 +575,8 @@ def hisa_page_tables(ctx_len: torch.Tensor, new_len: torch.Tensor, block_table: 
     if rows < 1:
         raise ValueError(f"rows: {rows}")
     if out is None:
-        out = PageTables.empty(n_seq, rows, device, key_rows=s_max > 0)
+        with _allocating(stream, device):
+            out = PageTables.empty(n_seq, rows, device, key_rows=s_max > 0)
     st = _call(lib().hisa_page_tables, dev, stream, ctx_len.data_ptr(), new_len.data_ptr(), n_seq, block_table.data_ptr(),
                block_table.shape[1], page, free_pages.data_ptr(), n_free, rows, s_max,
                *out.pointers(n_seq, rows, dev, device))
@@ -622,18 +635,21 @@ def _attention(name: str, queries: Queries, cache: Cache, index: torch.Tensor, k
             _fits(t, torch.int32, rows, dev) or _need(t, what, _I32, rows, device)
         ptrs.append(None if t is None else t.data_ptr())
     if out is None:
-        out = torch.empty_like(q)
+        with _allocating(stream, device):
+            out = torch.empty_like(q)
     else:
         _fits(out, dtype, q.shape, dev) or _need(out, "out", (dtype,), q.shape, device)
     if lse is not None:
         _fits(lse, torch.float32, (T, H), dev) or _need(lse, "lse", _F32, (T, H), device)
     elif want_lse:
-        lse = torch.empty((T, H), dtype=torch.float32, device=device)
+        with _allocating(stream, device):
+            lse = torch.empty((T, H), dtype=torch.float32, device=device)
     qc, cc = _Queries(q.data_ptr(), None, *ptrs, T, H, 0, queries.dtype), cache.c()
     L = lib()
     if ws is None:
         size = int(L.hisa_attention_workspace_bytes(qc, cc, k))
-        ws = torch.empty(size, dtype=torch.uint8, device=device) if size else None
+        with _allocating(stream, device):
+            ws = torch.empty(size, dtype=torch.uint8, device=device) if size else None
     else:
         size = ws.numel()
         _fits(ws, torch.uint8, ws.shape, dev) or _need(ws, "ws", (torch.uint8,), None, device)

@@ -124,3 +124,28 @@ def test_nothing_beside_the_outputs_and_the_workspace_is_written(kv, d, lens, H,
         want = (hisa.hisa_sparse_attention(b.queries, b.cache, lists) if k
                 else hisa.hisa_paged_attention(b.queries, b.cache, b.q_start))[0]
         assert torch.equal(out, want)
+
+
+@pytest.mark.parametrize("how", ["stream", "handle", "default"])
+def test_what_a_call_allocates_belongs_to_its_stream(how, monkeypatch):
+    b = Batch([(3000, 1), (70, 1)], seed=2)
+    b.queries.q_pos = b.put(b.pos)
+    want, wlse = hisa.hisa_paged_attention(b.queries, b.cache, b.q_start, want_lse=True)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    stream, handle = {"stream": (side, side.cuda_stream), "handle": (side.cuda_stream, side.cuda_stream), "default": (0, 0)}[how]
+    seen = []
+    for name in ("empty", "empty_like"):
+        real = getattr(torch, name)
+        monkeypatch.setattr(torch, name, lambda *a, real=real, **kw: seen.append(torch.cuda.current_stream().cuda_stream)
+                            or real(*a, **kw))
+    with torch.cuda.stream(torch.cuda.Stream()):                     # (the caller's own stream is a third one)
+        out, lse = hisa.hisa_paged_attention(b.queries, b.cache, b.q_start, want_lse=True, stream=stream)
+        ctx, new = b.put([3000, 70]), b.put([1, 1])
+        torch.cuda.synchronize()
+        before = len(seen)
+        assert seen == [handle] * before and before == 3             # out, lse, workspace
+        t = hisa.hisa_page_tables(ctx, new, b.cache.block_table.clone(), b.page, b.put([0] * 9), 2, stream=stream)
+        assert seen == [handle] * len(seen) and len(seen) > before
+    torch.cuda.synchronize()
+    assert torch.equal(out, want) and torch.equal(lse, wlse) and t.seq_len.tolist() == [3001, 71]
