@@ -390,7 +390,8 @@ def _need(t, name: str, dtypes, shape=None, device=None, contiguous: bool = True
 
 def _fits(t, dtype, shape, dev: int) -> bool:
     """What _need asks of a tensor, in one go: most calls pass, and a small call's time is its host side."""
-    return isinstance(t, torch.Tensor) and t.dtype is dtype and t.shape == shape and t.get_device() == dev and t.is_contiguous()
+    return (isinstance(t, torch.Tensor) and t.dtype is dtype and (shape is None or t.shape == shape)
+            and t.get_device() == dev and t.is_contiguous())
 
 
 def _gpu_of(t, name: str) -> int:
@@ -402,6 +403,7 @@ def _gpu_of(t, name: str) -> int:
     return t.get_device()
 
 
+_numel, _data_ptr = torch.Tensor.numel, torch.Tensor.data_ptr
 _I32 = (torch.int32,)
 _F32 = (torch.float32,)
 _STORED = {HISA_F32: (torch.float32,), HISA_BF16: (torch.bfloat16,),
@@ -530,17 +532,14 @@ class PageTables:
     def pointers(self, n_seq: int, rows: int, dev: int, device) -> list:
         """Where the seven tensors lie.  Their types and layout are checked once for a batch's sizes, and again if a
         tensor is replaced or resized."""
-        tensors = (self.seq_len, self.q_start, self.page_start, self.q_seq, self.q_pos, self.slots, self.key_rows)
-        sizes = (n_seq, n_seq + 1, n_seq + 1, rows, rows, rows, rows)
-        if (self.__dict__.get("_checked") != (n_seq, rows, dev)
-                or any([t is not None and t.numel() != n for t, n in zip(tensors, sizes)])):
-            names = ("seq_len", "q_start", "page_start", "q_seq", "q_pos", "slots")
-            for name, t, n in zip(names, tensors, sizes):
-                _need(t, name, _I32, (n,), device)
-            if self.key_rows is not None:
-                _need(self.key_rows, "key_rows", _I32, (rows,), device)
-            self.__dict__["_checked"] = (n_seq, rows, dev)
-        return [None if t is None else t.data_ptr() for t in tensors]
+        checked = self.__dict__.get("_checked")
+        if checked is None or checked[0] != (n_seq, rows, dev) or tuple(map(_numel, checked[1])) != checked[2]:
+            names = ("seq_len", "q_start", "page_start", "q_seq", "q_pos", "slots", "key_rows")[:6 + (self.key_rows is not None)]
+            sizes = (n_seq, n_seq + 1, n_seq + 1, rows, rows, rows, rows)[:len(names)]
+            tensors = tuple(_need(getattr(self, name), name, _I32, (n,), device) for name, n in zip(names, sizes))
+            checked = self.__dict__["_checked"] = ((n_seq, rows, dev), tensors, sizes)
+        lie = list(map(_data_ptr, checked[1]))
+        return lie if len(lie) == 7 else lie + [None]
 
     @property
     def pages_used(self) -> torch.Tensor:
@@ -571,7 +570,7 @@ def hisa_page_tables(ctx_len: torch.Tensor, new_len: torch.Tensor, block_table: 
     _fits(free_pages, i32, (n_free,), dev) or _need(free_pages, "free_pages", _I32, (n_free,), device)
     if block_table.dim() != 2 or block_table.shape[0] != n_seq:
         raise ValueError(f"block_table: shape {tuple(block_table.shape)}, needed is [{n_seq}, max_pages]")
-    _fits(block_table, i32, block_table.shape, dev) or _need(block_table, "block_table", _I32, None, device)
+    _fits(block_table, i32, None, dev) or _need(block_table, "block_table", _I32, None, device)
     if rows < 1:
         raise ValueError(f"rows: {rows}")
     if out is None:
@@ -625,7 +624,7 @@ def _attention(name: str, queries: Queries, cache: Cache, index: torch.Tensor, k
     q, ck = queries.q, cache.k
     dev, device = _gpu_of(ck, "k"), ck.device
     dtype = torch.float32 if queries.dtype == HISA_F32 else torch.bfloat16
-    _fits(q, dtype, q.shape, dev) or _need(q, "q", (dtype,), None, device)
+    _fits(q, dtype, None, dev) or _need(q, "q", (dtype,), None, device)
     if q.dim() != 3 or q.shape[2] != ck.shape[3]:
         raise ValueError(f"q: shape {tuple(q.shape)}, needed is [T, H, {ck.shape[3]}]")
     T, H, d = q.shape
@@ -652,7 +651,7 @@ def _attention(name: str, queries: Queries, cache: Cache, index: torch.Tensor, k
             ws = torch.empty(size, dtype=torch.uint8, device=device) if size else None
     else:
         size = ws.numel()
-        _fits(ws, torch.uint8, ws.shape, dev) or _need(ws, "ws", (torch.uint8,), None, device)
+        _fits(ws, torch.uint8, None, dev) or _need(ws, "ws", (torch.uint8,), None, device)
     scale = d ** -0.5 if scale is None else float(scale)
     ptrs = (scale, out.data_ptr(), None if lse is None else lse.data_ptr(), None if ws is None else ws.data_ptr(), size)
     if k:
@@ -682,7 +681,7 @@ def hisa_sparse_attention(queries: Queries, cache: Cache, topk_idx: torch.Tensor
     skipped).  Returns (out [T, H, d], lse [T, H] or None)."""
     if cache.block_table is None or cache.seq_len is None or cache.v is None:
         raise ValueError("cache: values, block_table and seq_len are needed")
-    _fits(topk_idx, torch.int32, topk_idx.shape, cache.k.get_device()) or _need(topk_idx, "topk_idx", _I32, None,
+    _fits(topk_idx, torch.int32, None, cache.k.get_device()) or _need(topk_idx, "topk_idx", _I32, None,
                                                                                  cache.k.device)
     if topk_idx.dim() != 2 or topk_idx.shape[0] != queries.T or topk_idx.shape[1] < 1:
         raise ValueError(f"topk_idx: shape {tuple(topk_idx.shape)}, needed is [{queries.T}, k]")
