@@ -773,7 +773,7 @@ static __global__ __launch_bounds__(256, D > 128 ? 1 : 2) void k_attn_f32(AttnAr
 // heads, so that wider groups gather every row once and still leave each SIMD two waves.  All rows see the same keys, so a
 // row outside is a row of zeros and a score of -inf for everybody.  Bound by memory: 4 D bytes (bf16) per key and KV head,
 // whatever the number of heads.  Measured, d = 128: one token of 32 sequences of up to 131072, 64 heads on 8 KV heads, 2.54
-// ms, 5.9 TB/s; of 200 short ones, 4 KV heads, fp8, 0.47 ms, 4.8 TB/s (a workgroup there is a quarter start and end); 1024
+// ms, 5.9 TB/s; of 200 short ones, 4 KV heads, fp8, 0.45 ms, 5.0 TB/s (a workgroup there is a quarter start and end); 1024
 // lists of 2048, 64 heads on one KV head, 136 us (8 TB/s gathered, from L2 for the most part).
 constexpr int kRowWaves = 4;
 
@@ -1027,7 +1027,7 @@ static __global__ __launch_bounds__(PAIR ? 512 : 256, 2) void k_attn_rows(AttnAr
 // ---- many rows per sequence ----------------------------------------------------------------------
 // A workgroup of 8 waves takes 256 query rows of one KV head (32 per wave) and a part of their keys, in tiles of 64 keys
 // that all waves multiply from LDS.  Bound by the matrix units (4 D flop per visible pair) and, for d = 64, by the vector
-// units that make the weights.  Measured: 1024 tokens behind 64K, 64 heads on 8, d = 128, 2.05 ms, 1.06 PFLOP/s (fp8 2.3 ms);
+// units that make the weights.  Measured: 1024 tokens behind 64K, 64 heads on 8, d = 128, 2.0 ms, 1.1 PFLOP/s (fp8 2.3 ms);
 // eleven prompts of 2777 tokens at most, windows of 1024, 32 heads on 2, d = 64, fp8, 0.53 ms, 0.42.  Each SIMD holds two waves, one
 // of the first four (group 0) and one of the last four (group 1).  In interval i, between two barriers, group 0 turns its
 // scores of tile i into weights, then runs its products for tile i + 1 (scores of tile i + 1, values of tile i), while
