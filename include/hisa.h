@@ -243,6 +243,16 @@ int hisa_index_iou(const int32_t* a_idx, const int32_t* b_idx, int32_t T, int32_
  * ---------------------------------------------------------------------------------------------- */
 
 /*
+ * What the attention over a BF16 or FP8 cache multiplies with its values (the sums of weights are fp32 either way):
+ *   HISA_WEIGHTS_16BIT  (0) two bf16 parts of each weight, 16 bits together: a result is off by little more than its
+ *                       own rounding to bf16
+ *   HISA_WEIGHTS_8BIT   one bf16, 8 bits: a result of many keys is off by up to 1.45 times that in the mean square.
+ *                       For prompts, where the second part costs a fifth to a third of the call; single tokens wait
+ *                       for memory and gain nothing
+ */
+typedef enum { HISA_WEIGHTS_16BIT = 0, HISA_WEIGHTS_8BIT = 1 } hisa_weights;
+
+/*
  * A cache of n_pages pages of `page` token rows each, H_kv heads of d elements per row.  Row (page p,
  * offset o, head h) begins page_stride * p + token_stride * o + head_stride * h elements behind k and
  * behind v (one set of strides for both, so [n_pages, page, H_kv, d], [n_pages, H_kv, page, d] and
@@ -264,6 +274,7 @@ typedef struct {
   int32_t        H_kv;
   int32_t        d;
   int32_t        dtype;       /* hisa_dtype                                                            */
+  int32_t        weights;     /* hisa_weights: of the attention over a BF16 or FP8 cache                */
 } hisa_cache;
 
 /*
@@ -333,8 +344,8 @@ int hisa_cache_append(const hisa_cache* cache, const int32_t* slots, const void*
  * scale positive and finite.  A launch holds fewer than 2^23 workgroups: split larger calls.  What always
  * fits: T * H_kv * ceil(H / H_kv / 32) below that (lists), T * H / 32 + 4 * n_seq * H_kv (ranges).
  * Scores, the running maximum and sum and the output are held in fp32; for the second product (bf16 and
- * fp8 caches) the weights p_s are rounded to bf16, where T * H <= 1024 to two bf16 parts (16 bits).  All
- * sums have a fixed order: the same call gives the same bits.
+ * fp8 caches) the weights p_s are rounded as cache->weights says.  All sums have a fixed order: the same
+ * call gives the same bits.
  * Workspace: hisa_attention_workspace_bytes(queries, cache, 0), which depends on shapes only.
  */
 int hisa_paged_attention(const hisa_queries* queries, const hisa_cache* cache, const int32_t* q_start,

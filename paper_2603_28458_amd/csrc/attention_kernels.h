@@ -220,8 +220,9 @@ __device__ __forceinline__ void scale_scores(f32x16 (&s)[NB], const float* ks) {
 
 // Scores of NB blocks of 32 keys -> weights as B operands; updates m, l, o.  vs: scales of the value rows (fp8).
 // A weight rounded to bf16 is off by up to 2^-8 of itself (1.6e-3 in the mean square), and so are the sums: as much as the
-// result's own rounding adds.  REST: what is left of each weight goes to `rest`, for a second product of the values,
-// with which the sums are as good as with weights in fp32 (to 2^-16).  It is cut and not rounded off, so that both parts have
+// result's own rounding adds, and more where few rows leave it no chance to average out (7 rows up to 1.7 times, 1024 rows
+// 1.45).  A caller may choose that.  REST, which is what one gets otherwise: what is left of each weight goes to `rest`, for a
+// second product of the values, with which the sums are as good as with weights in fp32 (to 2^-15).  It is cut and not rounded off, so that both parts have
 // one sign, and never 0 where there is a weight: an infinite value stays what it is in both products.
 __device__ __forceinline__ float cut_off(float w, uint32_t bits) {
   return __builtin_amdgcn_fmed3f(w - __uint_as_float(bits & 0xffff0000u), w, 1.17549435e-38f);
@@ -774,7 +775,7 @@ static __global__ __launch_bounds__(256, D > 128 ? 1 : 2) void k_attn_f32(AttnAr
 // row outside is a row of zeros and a score of -inf for everybody.  Bound by memory: 4 D bytes (bf16) per key and KV head,
 // whatever the number of heads.  Measured, d = 128: one token of 32 sequences of up to 131072, 64 heads on 8 KV heads, 2.54
 // ms, 5.9 TB/s; of 200 short ones, 4 KV heads, fp8, 0.45 ms, 5.0 TB/s (a workgroup there is a quarter start and end); 1024
-// lists of 2048, 64 heads on one KV head, 136 us (8 TB/s gathered, from L2 for the most part).
+// lists of 2048, 64 heads on one KV head, 157 us (6.8 TB/s gathered, from L2 for the most part; weights of 8 bits 137).
 constexpr int kRowWaves = 4;
 
 template <int D, int KDT, bool PAIR>
@@ -1027,8 +1028,9 @@ static __global__ __launch_bounds__(PAIR ? 512 : 256, 2) void k_attn_rows(AttnAr
 // ---- many rows per sequence ----------------------------------------------------------------------
 // A workgroup of 8 waves takes 256 query rows of one KV head (32 per wave) and a part of their keys, in tiles of 64 keys
 // that all waves multiply from LDS.  Bound by the matrix units (4 D flop per visible pair) and, for d = 64, by the vector
-// units that make the weights.  Measured: 1024 tokens behind 64K, 64 heads on 8, d = 128, 2.0 ms, 1.1 PFLOP/s (fp8 2.3 ms);
-// eleven prompts of 2777 tokens at most, windows of 1024, 32 heads on 2, d = 64, fp8, 0.53 ms, 0.42.  Each SIMD holds two waves, one
+// units that make the weights; a second part of the weights (REST) is half as many products again.  Measured: 1024 tokens
+// behind 64K, 64 heads on 8, d = 128, 2.7 ms, 0.81 PFLOP/s (fp8 3.0 ms; weights of 8 bits 2.0 and 2.3 ms); eleven prompts of 2777
+// tokens at most, windows of 1024, 32 heads on 2, d = 64, fp8, 0.63 ms, 0.36 (8 bits 0.52).  Each SIMD holds two waves, one
 // of the first four (group 0) and one of the last four (group 1).  In interval i, between two barriers, group 0 turns its
 // scores of tile i into weights, then runs its products for tile i + 1 (scores of tile i + 1, values of tile i), while
 // group 1 runs its products for tile i, then turns those scores into weights: one computes while the other multiplies, and

@@ -46,6 +46,7 @@ int check_attention(const hisa_queries* q, const hisa_cache* c, int32_t k) {
   if (c->n_seq < 1 || c->n_seq > kMaxSeq || c->max_pages < 1 || q->H % c->H_kv) return HISA_ERR_SHAPE;
   if (c->page & (c->page - 1) || overflows31(c->max_pages, c->page)) return HISA_ERR_SHAPE;
   if (k < 0 || k > kMaxList) return HISA_ERR_SHAPE;
+  if (c->weights != HISA_WEIGHTS_16BIT && c->weights != HISA_WEIGHTS_8BIT) return HISA_ERR_DTYPE;
   if (q->q_dtype == HISA_F32 && c->dtype == HISA_F32) {
     if (c->d < 4 || c->d % 4 || c->d > kF32MaxD) return HISA_ERR_SHAPE;
   } else if (q->q_dtype == HISA_BF16 && (c->dtype == HISA_BF16 || c->dtype == HISA_FP8_E4M3)) {
@@ -62,7 +63,7 @@ enum AttnKernel { ATTN_F32, ATTN_ROWS, ATTN_CHUNK };
 struct AttnPlan {
   AttnKernel kernel;
   bool pair;          // ATTN_ROWS: 64 heads per workgroup, not 32
-  bool rest;          // bf16, fp8: weights in two parts
+  bool rest;          // bf16, fp8: weights in two parts (the caller's choice)
   long units;         // tiles of query rows, of one KV head
   int splits;         // parts of their keys
   size_t ws_bytes;
@@ -93,11 +94,10 @@ AttnPlan plan_attention(const hisa_queries* q, const hisa_cache* c, int32_t k) {
   const long keys = k ? k : (long)c->max_pages * c->page;
   const long G = q->H / c->H_kv, T = q->T;
   long most = (keys + kPartKeys - 1) / kPartKeys, splits;
-  // Weights to 16 bits and not to 8 where there are few rows: rounding errors of random sign do not average out over those
-  // (the mean square error of 7 rows was up to 1.7 times that of a rounded result, of 1024 rows 1.45 times; with it 1.00),
-  // and such a call waits for other things than the second product (one token over 130K keys 115 and 116 us, 16 lists of
-  // 2048 15.6 and 16.1).  With many rows it costs what a product costs (1024 lists of 2048 145 and 163 us).
-  p.rest = T * q->H <= 1024;
+  // The second part costs nothing where a call waits for memory (32 tokens over up to 131072 keys 2563 and 2570 us, 1 over
+  // 1000 12.6 and 12.5, 32 lists of 2048 19.8 and 20.4), and what a product costs where there are many rows: 1024 lists of
+  // 2048 137 and 157 us, 1024 tokens behind 64K 1.95 and 2.68 ms, fp8 2.30 and 2.96.
+  p.rest = c->weights == HISA_WEIGHTS_16BIT;
   // A few new tokens a sequence: one at a time reads their keys that many times, from L2 for the most part, with every
   // wave on keys of its own; together they read them once, but 32 rows are one wave's, and a tile of 64 keys takes it
   // 4000 cycles from scores to values.  Measured, 64 sequences of 3000, 2 new tokens each: 145 us one at a time, 200

@@ -15,6 +15,7 @@ from typing import Optional
 import torch
 
 HISA_F32, HISA_BF16, HISA_FP8_E4M3 = 0, 1, 2
+HISA_WEIGHTS_16BIT, HISA_WEIGHTS_8BIT = 0, 1
 OP_POOL, OP_BLOCK_SCORE_TOPK, OP_TOKEN_REFINE_TOPK, OP_FLAT_TOPK = 0, 1, 2, 3
 DTYPE_CODE = {"f32": HISA_F32, "bf16": HISA_BF16, "fp8_e4m3": HISA_FP8_E4M3}
 LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "lib", "libhisa.so")
@@ -49,7 +50,7 @@ class _Cache(C.Structure):
                 ("block_table", C.c_void_p), ("seq_len", C.c_void_p), ("page_stride", C.c_int64),
                 ("token_stride", C.c_int64), ("head_stride", C.c_int64), ("n_pages", C.c_int32), ("page", C.c_int32),
                 ("n_seq", C.c_int32), ("max_pages", C.c_int32), ("H_kv", C.c_int32), ("d", C.c_int32),
-                ("dtype", C.c_int32)]
+                ("dtype", C.c_int32), ("weights", C.c_int32)]
 
 
 _lib = None
@@ -450,7 +451,8 @@ class Cache:
     """A paged cache: k, v [n_pages, page, H_kv, d] (float32 / bfloat16 / uint8 or float8 codes; any strides that k and v
     share, the last dimension contiguous, so a transposed [n_pages, H_kv, page, d] or a slice of an array that holds both
     fits), k_scale / v_scale [n_pages, page, H_kv] float32 for fp8, block_table [n_seq, max_pages] and seq_len [n_seq]
-    int32; all on the GPU.  v None: keys alone, block_table and seq_len None: to append to only."""
+    int32; all on the GPU.  v None: keys alone, block_table and seq_len None: to append to only.  weights: what the attention
+    rounds its weights to (bf16 and fp8 caches): 16 bits, or 8, which is faster where prompts are long."""
     k: torch.Tensor
     v: Optional[torch.Tensor]
     dtype: int
@@ -458,6 +460,7 @@ class Cache:
     seq_len: Optional[torch.Tensor] = None
     k_scale: Optional[torch.Tensor] = None
     v_scale: Optional[torch.Tensor] = None
+    weights: int = HISA_WEIGHTS_16BIT
 
     def __setattr__(self, name, value):
         object.__setattr__(self, name, value)
@@ -472,6 +475,8 @@ class Cache:
     def check(self):
         if self.dtype not in _STORED:
             raise ValueError(f"dtype: unknown code {self.dtype}")
+        if self.weights not in (HISA_WEIGHTS_16BIT, HISA_WEIGHTS_8BIT):
+            raise ValueError(f"weights: unknown code {self.weights}")
         if self.k.dim() != 4:
             raise ValueError(f"k: shape {tuple(self.k.shape)}, needed is [n_pages, page, H_kv, d]")
         dev = self.k.device
@@ -501,7 +506,7 @@ class Cache:
             self.check()
             n_seq, max_pages = laid[2] or (0, 0)
             c = _Cache(None, None, None, None, None, None, *laid[1][:3], *laid[0][:2], n_seq, max_pages, *laid[0][2:],
-                       self.dtype)
+                       self.dtype, self.weights)
             self.__dict__.update(_laid=laid, _c=c)
         # The sizes stay while the tensors keep theirs (the struct costs 3 us to build); where memory lies is asked anew.
         c.k = k.data_ptr()

@@ -280,3 +280,20 @@ def test_the_oracle():
     assert np.allclose(out[0, 0], [(5 + 2 + 6) / 5, (6 + 4 - 8) / 5]) and np.isclose(lse[0, 0], np.log(5.0))
     assert np.allclose(mag[0, 0], [(5 + 2 + 6) / 5, (6 + 4 + 8) / 5])
     assert out[1, 0].tolist() == [0, 0] and np.isneginf(lse[1, 0]) and np.isnan(lse[2, 0])
+
+
+# ---- what the attention rounds its weights to
+@pytest.mark.parametrize("weights", [-1, 2, 7])
+def test_unknown_weights_are_refused(lib, monkeypatch, weights):  # noqa: F811
+    assert paged(lib, queries(), cache(weights=weights)) == DTYPE and sparse(lib, queries(), cache(weights=weights)) == DTYPE
+    monkeypatch.setattr(hisa, "_on_gpu", lambda t: True)
+    k = torch.zeros((2, 4, 2, 64), dtype=torch.bfloat16)
+    with pytest.raises(ValueError, match="weights"):
+        hisa.Cache(k=k, v=k, dtype=BF16, weights=weights)
+    c = hisa.Cache(k=k, v=k, dtype=BF16)
+    assert c.c().weights == hisa.HISA_WEIGHTS_16BIT and C.sizeof(hisa._Cache) == 104
+    c.weights = hisa.HISA_WEIGHTS_8BIT
+    assert c.c().weights == hisa.HISA_WEIGHTS_8BIT
+    c.weights = weights
+    with pytest.raises(ValueError, match="weights"):
+        c.c()
