@@ -283,7 +283,8 @@ typedef struct {
  * stand in `rows` token rows, sequence after sequence.  All arrays are device arrays.
  *   block_table [n_seq, max_pages] in/out: the entries ceil(ctx_len/page) .. ceil((ctx_len+new_len)/page)
  *               - 1 of each sequence are taken from free_pages, in the order of the sequences; every
- *               other entry is left as it was
+ *               other entry is left as it was.  New tokens beyond the last of `rows` get their pages all
+ *               the same (and count in seq_len), only no row and no slot
  *   free_pages  [n_free] page ids; the first page_start[n_seq] of them are in use afterwards.  If that
  *               number exceeds n_free, the entries beyond are written as -1 and their tokens get no slot
  *   seq_len     [n_seq] out: ctx_len + new_len, at most max_pages * page
@@ -329,7 +330,8 @@ int hisa_cache_append(const hisa_cache* cache, const int32_t* slots, const void*
  * where k_s, v_s are the rows of KV head h / (H / H_kv).  Nothing at a position that a query does not
  * see affects its result, infinities and NaN included.  A query that sees no key gives zeros and -inf.
  *   queries     q [T, H, d], T, H, q_dtype; q_pos (NULL: the new tokens are the last q_start[n+1] -
- *               q_start[n] positions of their sequence) and q_lo (NULL: 0) as everywhere.  A document
+ *               q_start[n] positions of their sequence, which is not so where hisa_page_tables had more new
+ *               tokens than rows: its q_pos is right there too) and q_lo (NULL: 0) as everywhere.  A document
  *               or sliding-window mask is a q_lo, a prefix that sees itself whole a q_pos beyond the
  *               own position.  w, q_seq and q_pos0 are not read
  *   q_start     [n_seq + 1] first token row of each sequence, ascending (device, in), as

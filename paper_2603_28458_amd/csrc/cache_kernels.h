@@ -101,16 +101,23 @@ __device__ __forceinline__ int table_find(const Start& start, int n_seq, int x) 
   return lo;
 }
 
-// Token row e, and page e of those taken from the free list (a new page holds a new token, so there are at most `rows`).
+// Pages taken from the free list, from number `first` on, every `step`-th.  (Where all new tokens have a row there are no
+// more of them than rows, and threads: a new page holds a new token.  Where `rows` cuts the tokens short there may be any
+// number, and each thread takes several.)
 template <class Start>
-__device__ __forceinline__ void table_row(const TableArgs& a, const Start& q_start, const Start& page_start, int tokens,
-                                          int pages, int e) {
-  if (e < pages) {
-    const int n = table_find(page_start, a.n_seq, e);
+__device__ __forceinline__ void table_pages(const TableArgs& a, const Start& page_start, int pages, uint32_t first,
+                                            uint32_t step) {
+  for (uint32_t e = first; e < (uint32_t)pages; e += step) {          // (both below 2^31)
+    const int n = table_find(page_start, a.n_seq, (int)e);
     const TableSeq s = table_seq(a, n);
-    const int j = s.had + e - (int)page_start[n];
-    if (j < s.need) a.block_table[(long)n * a.max_pages + j] = e < a.n_free ? a.free_pages[e] : -1;
+    const int j = s.had + (int)e - (int)page_start[n];
+    if (j < s.need) a.block_table[(long)n * a.max_pages + j] = (int)e < a.n_free ? a.free_pages[e] : -1;
   }
+}
+
+// Token row e.
+template <class Start>
+__device__ __forceinline__ void table_row(const TableArgs& a, const Start& q_start, const Start& page_start, int tokens, int e) {
   if (e >= a.rows) return;
   int seq = 0, pos = -1, slot = -1, key_row = -1;
   if (e < tokens) {
@@ -159,7 +166,9 @@ static __global__ __launch_bounds__(kTableThreads) void k_page_tables(TableArgs 
     }
   }
   __syncthreads();
-  table_row(a, q_start, page_start, (int)tok_all, (int)pg_all, blockIdx.x * kTableThreads + n);
+  const int e = blockIdx.x * kTableThreads + n;
+  table_pages(a, page_start, (int)pg_all, e, gridDim.x * kTableThreads);
+  table_row(a, q_start, page_start, (int)tok_all, e);
 }
 
 // More sequences: the scans by one workgroup (each thread a run of consecutive sequences), the rows by another launch.
@@ -189,7 +198,9 @@ static __global__ __launch_bounds__(kTableThreads) void k_page_scan(TableArgs a)
 }
 
 static __global__ __launch_bounds__(256) void k_page_rows(TableArgs a) {
-  table_row(a, a.q_start, a.page_start, a.q_start[a.n_seq], a.page_start[a.n_seq], blockIdx.x * 256 + threadIdx.x);
+  const int e = blockIdx.x * 256 + threadIdx.x;
+  table_pages(a, a.page_start, a.page_start[a.n_seq], e, gridDim.x * 256);
+  table_row(a, a.q_start, a.page_start, a.q_start[a.n_seq], e);
 }
 
 // ---- new rows into the cache --------------------------------------------------------------------

@@ -114,3 +114,17 @@ def test_without_an_output_given():
     assert t.key_rows is None and t.slots.tolist() == [77, 24, 25, 26, -1, -1]
     t = hisa.hisa_page_tables(ctx, new, table, 8, torch.tensor([3, 4], dtype=torch.int32, device=dev), 6, s_max=32)
     assert t.key_rows.tolist() == [5, 32, 33, 34, -1, -1] and t.q_seq.tolist() == [0, 1, 1, 1, 0, 0]
+
+
+@pytest.mark.parametrize("n_seq,new,page,rows,n_free", [
+    (4, 2000, 1, 1000, None), (1, 5000, 1, 100, None), (1, 32000, 16, 512, None), (32, 4096, 16, 4096, None),
+    (4, 2000, 1, 1000, 5000), (3, 1025, 1, 1, None),
+    (2000, 160, 16, 8192, None), (2000, 160, 16, 8192, 12345), (1100, 7, 1, 1, None), (1025, 300, 7, 257, 40000)])
+def test_more_new_pages_than_rows(n_seq, new, page, rows, n_free):
+    """Every page of every new token is taken and named, whether the token has a row or not; in one launch and in two."""
+    ctx = np.arange(n_seq) * 7 % 50
+    run(ctx, np.full(n_seq, new), (new + 50) // page + 2, page, rows, n_free=n_free, seed=n_seq)
+    # some sequences grow far past the rows, others not at all
+    g = np.random.default_rng(n_seq)
+    some = np.where(g.random(n_seq) < 0.4, 0, g.integers(0, 2 * new, n_seq))
+    run(ctx, some, (new + 50) // page + 2, page, rows, n_free=n_free, s_max=64, seed=n_seq + 1)
