@@ -22,10 +22,9 @@ struct TableArgs {
 };
 
 constexpr int kTableThreads = 1024;
-constexpr uint32_t kPageCap = 1u << 30;   // where the count of pages taken stops (two of them still fit 32 bits)
 
-// A sequence as the tables see it: lengths that cannot lead out of any array.  Sums of new tokens stop at `rows` and sums
-// of pages at kPageCap: adding with a ceiling is associative, so a scan may do it in any order.
+// A sequence as the tables see it: lengths that cannot lead out of any array.  Sums of new tokens stop at `rows`: adding
+// with a ceiling is associative, so a scan may do it in any order.  Sums of pages stay below n_seq * max_pages, so 2^31.
 struct TableSeq {
   int ctx, had, need;     // tokens cached, pages they fill, pages they and the new ones fill
   uint32_t fresh, grown;  // new tokens, new pages
@@ -53,7 +52,7 @@ __device__ __forceinline__ uint32_t add_to(uint32_t a, uint32_t b, uint32_t ceil
   return s < ceiling ? s : ceiling;
 }
 
-// Exclusive prefix sums (with ceilings) of one value pair per thread over the workgroup; the totals come back too.
+// Exclusive prefix sums (of tokens with a ceiling) of one value pair per thread over the workgroup; the totals come back too.
 __device__ __forceinline__ void table_scan(uint32_t& tok, uint32_t& pg, uint32_t& tok_all, uint32_t& pg_all,
                                            uint32_t ceiling, uint32_t (*part)[2]) {
   const int lane = lane_id(), wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
@@ -63,7 +62,7 @@ __device__ __forceinline__ void table_scan(uint32_t& tok, uint32_t& pg, uint32_t
     const uint32_t tu = __shfl_up(t, o), pu = __shfl_up(p, o);
     if (lane >= o) {
       t = add_to(t, tu, ceiling);
-      p = add_to(p, pu, kPageCap);
+      p += pu;
     }
   }
   if (lane == 63) {
@@ -80,11 +79,11 @@ __device__ __forceinline__ void table_scan(uint32_t& tok, uint32_t& pg, uint32_t
       pb = pa;
     }
     ta = add_to(ta, part[w][0], ceiling);
-    pa = add_to(pa, part[w][1], kPageCap);
+    pa += part[w][1];
   }
   __syncthreads();
   tok = add_to(tb, te, ceiling);
-  pg = add_to(pb, pe, kPageCap);
+  pg = pb + pe;
   tok_all = ta;
   pg_all = pa;
 }
@@ -180,7 +179,7 @@ static __global__ __launch_bounds__(kTableThreads) void k_page_scan(TableArgs a)
   for (int n = first; n < last; ++n) {
     const TableSeq s = table_seq(a, n);
     tok = add_to(tok, s.fresh, (uint32_t)a.rows);
-    pg = add_to(pg, s.grown, kPageCap);
+    pg += s.grown;
   }
   table_scan(tok, pg, tok_all, pg_all, (uint32_t)a.rows, part);
   for (int n = first; n < last; ++n) {
@@ -189,7 +188,7 @@ static __global__ __launch_bounds__(kTableThreads) void k_page_scan(TableArgs a)
     a.q_start[n] = (int)tok;
     a.page_start[n] = (int)pg;
     tok = add_to(tok, s.fresh, (uint32_t)a.rows);
-    pg = add_to(pg, s.grown, kPageCap);
+    pg += s.grown;
   }
   if (threadIdx.x == 0) {
     a.q_start[a.n_seq] = (int)tok_all;

@@ -128,3 +128,22 @@ def test_more_new_pages_than_rows(n_seq, new, page, rows, n_free):
     g = np.random.default_rng(n_seq)
     some = np.where(g.random(n_seq) < 0.4, 0, g.integers(0, 2 * new, n_seq))
     run(ctx, some, (new + 50) // page + 2, page, rows, n_free=n_free, s_max=64, seed=n_seq + 1)
+
+
+@pytest.mark.parametrize("n_seq", [1, 1025])
+def test_more_than_a_billion_new_pages(n_seq):
+    """A table of more than 2^30 entries, all of them new."""
+    dev = torch.device("cuda:0")
+    most = (2 ** 30 + 12345) // n_seq
+    table = torch.full((n_seq, most + 1), 7, dtype=torch.int32, device=dev)
+    length = torch.full((n_seq,), most, dtype=torch.int32, device=dev)
+    free = torch.tensor([11, 12, 13], dtype=torch.int32, device=dev)
+    if n_seq > 1:
+        length[0] += 1                                              # (into the last column)
+    total = int(length.long().sum())
+    assert total > 2 ** 30
+    t = hisa.hisa_page_tables(torch.zeros_like(length), length, table, 1, free, 1 << 22)
+    torch.cuda.synchronize()
+    assert int(t.pages_used) == total and torch.equal(t.seq_len, length)
+    assert table[0, :3].tolist() == [11, 12, 13] and int((table == -1).sum()) == total - 3
+    assert int((table == 7).sum()) == n_seq * (most + 1) - total and int(table[-1, -1]) == 7
