@@ -565,7 +565,7 @@ static __global__ __launch_bounds__(256, D > 128 ? 1 : 2) void k_attn_f32(AttnAr
     lo_min = wave_min_int(seen.lo);
     lo_max = wave_max_int(seen.lo);
     begin = lo_min >> 5;
-    end = (pos_max + 32) >> 5;
+    end = (pos_max >> 5) + 1;                                 // (a position may be the last one below 2^31)
     if (pos_max < 0 || end < begin) end = begin;
   }
   if (a.splits > 1) take_part(begin, end, split, a.splits, 4);   // of at least one tile per wave
@@ -838,7 +838,7 @@ static __global__ __launch_bounds__(PAIR ? 512 : 256, 2) void k_attn_rows(AttnAr
     pos = pos < len ? pos : len - 1;
     lo = q_lo > 0 ? q_lo : 0;
     begin = lo >> 5;
-    end = (pos + 32) >> 5;
+    end = (pos >> 5) + 1;                       // (a position may be the last one below 2^31)
     if (pos < 0 || end < begin) end = begin;
   }
   if (a.splits > 1) take_part(begin, end, split, a.splits, 8);      // of at least two tiles per wave
@@ -1122,7 +1122,7 @@ static __global__ __launch_bounds__(512, 2) void k_attn_chunk(AttnArgs a) {
   wg_lo = wave_min_int(wg_lo);
   const int pos_min = wave_min_int(st.pos), lo_max = wave_max_int(st.lo);
 
-  int begin = wg_lo / kChunkKeys, end = (wg_pos + kChunkKeys) / kChunkKeys;
+  int begin = wg_lo / kChunkKeys, end = wg_pos / kChunkKeys + 1;
   if (wg_pos < 0 || end < begin) end = begin;
   if (a.splits > 1) {
     take_part(begin, end, split, a.splits, 4);
@@ -1138,15 +1138,17 @@ static __global__ __launch_bounds__(512, 2) void k_attn_chunk(AttnArgs a) {
   int* odd = slots + 8 * kChunkKeys;                                                   // [8]: tile with values dropped
   float* scales = reinterpret_cast<float*>(odd + 8);                                   // [8][2][64] (fp8)
   if (threadIdx.x < 8) odd[threadIdx.x] = -1;
+  // first position of a tile; of those behind the last one, which are asked about too, perhaps beyond 2^31 and negative
+  auto first_of = [](int tile) { return (int)((uint32_t)tile * kChunkKeys); };
   auto seen_row = [&](int tile) {            // of this lane
-    const int s = tile * kChunkKeys + lane;
+    const int s = first_of(tile) | lane;
     return tile < end && s >= wg_lo && s <= wg_pos;
   };
   auto page_entry = [&](int tile) {          // (an entry that there is, whatever the tile)
-    return table + (seen_row(tile) ? (tile * kChunkKeys + lane) >> a.page_shift : 0);
+    return table + (seen_row(tile) ? (first_of(tile) | lane) >> a.page_shift : 0);
   };
   auto publish = [&](int tile, int page) {
-    const int o = (tile * kChunkKeys + lane) & ((1 << a.page_shift) - 1);
+    const int o = (first_of(tile) | lane) & ((1 << a.page_shift) - 1);
     const bool ok = seen_row(tile) && (uint32_t)page < (uint32_t)a.n_pages;
     const uint64_t mask = __builtin_amdgcn_ballot_w64(ok);
     offsets[(tile & 7) * kChunkKeys + lane] = ok ? (page * a.page_stride + o * a.token_stride) * kBytes : -1;
@@ -1211,7 +1213,7 @@ static __global__ __launch_bounds__(512, 2) void k_attn_chunk(AttnArgs a) {
     else if (wave == 1) dma_left<n>();
     else dma_left<Geo::kPerThread>();
   };
-  auto mixed = [&](int tile) { return tile * kChunkKeys + kChunkKeys - 1 > wg_pos_min || tile * kChunkKeys < wg_lo_max; };
+  auto mixed = [&](int tile) { return (first_of(tile) | (kChunkKeys - 1)) > wg_pos_min || first_of(tile) < wg_lo_max; };
   // chunk i of an arrived step: cleared where its row is none, and of infinities and NaN in a mixed tile
   auto cleaned = [&](int i, uint4 x, uint64_t km, uint64_t vm, int tile) {
     if (!((is_value(i) ? vm : km) >> row_of(i) & 1)) x = make_uint4(0, 0, 0, 0);

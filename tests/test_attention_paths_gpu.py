@@ -149,3 +149,28 @@ def test_what_a_call_allocates_belongs_to_its_stream(how, monkeypatch):
         assert seen == [handle] * len(seen) and len(seen) > before
     torch.cuda.synchronize()
     assert torch.equal(out, want) and torch.equal(lse, wlse) and t.seq_len.tolist() == [3001, 71]
+
+
+@pytest.mark.parametrize("kv,d", [("bf16", 128), ("fp8", 64), ("f32", 36), ("f32", 128)])
+@pytest.mark.parametrize("new", [1, 3, 150])
+def test_sequences_that_end_at_the_last_position(kv, d, new):
+    """A table of 2^31 - 16 positions, of which the last 496 have pages: what is seen there is what a short sequence sees."""
+    b = Batch([(496 - new, new)], H=8, H_kv=2, d=d, kv=kv, page=16, seed=new + d)
+    lo = np.maximum(0, b.pos.astype(np.int64) - 99)
+    want = b.want(lambda t: np.arange(lo[t], int(b.pos[t]) + 1))
+    shift = 2 ** 31 - 512
+    table = torch.full((1, 2 ** 27 - 1), -1, dtype=torch.int32, device=b.dev)
+    table[0, shift // 16:] = b.cache.block_table[0, :31]
+    b.cache.block_table, b.cache.seq_len = table, b.put([2 ** 31 - 16])
+    b.queries.q_lo = b.put(lo + shift)
+    print(f"\n[last position] kv={kv} d={d} new={new}", flush=True)
+    for q_pos in (b.put(b.pos.astype(np.int64) + shift), None, b.put(np.full(b.T, 2 ** 31 - 1))):
+        b.queries.q_pos = q_pos
+        out, lse = hisa.hisa_paged_attention(b.queries, b.cache, b.q_start, want_lse=True)
+        torch.cuda.synchronize()
+        if q_pos is not None and int(q_pos[0]) == 2 ** 31 - 1:
+            want = b.want(lambda t: np.arange(lo[t], 496))
+        b.check(out, lse, want, 496, what="last position", weights=2.0 ** -15)
+    lists = lo[:, None] + np.arange(130)
+    out, lse = hisa.hisa_sparse_attention(b.queries, b.cache, b.put(lists + shift), want_lse=True)
+    b.check(out, lse, b.want(lambda t: lists[t]), 496, what="last position, lists", weights=2.0 ** -15)
