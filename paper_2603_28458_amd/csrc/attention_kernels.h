@@ -424,7 +424,7 @@ __device__ __forceinline__ Seen seen_by(const AttnArgs& a, int n, int len, int t
   Seen s;
   const int pos = a.q_pos ? a.q_pos[t] : a.seq_len[n] - t_end + t;
   const int lo = a.q_lo ? a.q_lo[t] : 0;
-  s.pos = pos < len ? pos : len - 1;
+  s.pos = pos < -1 ? -1 : pos < len ? pos : len - 1;     // (differences of positions fit 32 bits)
   s.lo = lo > 0 ? lo : 0;
   return s;
 }

@@ -174,3 +174,15 @@ def test_sequences_that_end_at_the_last_position(kv, d, new):
     lists = lo[:, None] + np.arange(130)
     out, lse = hisa.hisa_sparse_attention(b.queries, b.cache, b.put(lists + shift), want_lse=True)
     b.check(out, lse, b.want(lambda t: lists[t]), 496, what="last position, lists", weights=2.0 ** -15)
+
+
+@pytest.mark.parametrize("kv", ["bf16", "fp8", "f32"])
+@pytest.mark.parametrize("new", [1, 70])
+@pytest.mark.parametrize("far", [-2 ** 31, -2 ** 31 + 70, -2 ** 30, -2])
+def test_positions_far_before_the_first_see_nothing(kv, new, far):
+    """Beside rows of the same tile that see their prefix."""
+    b = Batch([(200, new), (0, new), (31, new)], H=8, H_kv=2, kv=kv, seed=new)
+    pos = b.pos.copy()
+    pos[::3] = far
+    out, lse = paged.run(b, positions=pos, what=f"position {far}")
+    assert (out[::3] == 0).all() and torch.isneginf(lse[::3]).all()
