@@ -404,7 +404,7 @@ def _gpu_of(t, name: str) -> int:
     return t.get_device()
 
 
-_numel, _data_ptr = torch.Tensor.numel, torch.Tensor.data_ptr
+_numel, _data_ptr, _is_contiguous = torch.Tensor.numel, torch.Tensor.data_ptr, torch.Tensor.is_contiguous
 _I32 = (torch.int32,)
 _F32 = (torch.float32,)
 _STORED = {HISA_F32: (torch.float32,), HISA_BF16: (torch.bfloat16,),
@@ -467,7 +467,7 @@ class Cache:
         self.__dict__.pop("_c", None)
 
     def __getstate__(self):  # (copies build a struct of their own)
-        return {name: value for name, value in self.__dict__.items() if name not in ("_c", "_laid")}
+        return {name: value for name, value in self.__dict__.items() if not name.startswith("_")}
 
     def __post_init__(self):
         self.check()
@@ -500,15 +500,18 @@ class Cache:
 
     def c(self) -> _Cache:
         k, v, ks, vs, table, length = self.k, self.v, self.k_scale, self.v_scale, self.block_table, self.seq_len
-        laid = (k.shape, k.stride(), None if table is None else table.shape)
+        laid = (k.shape, k.stride(), v is None or (v.shape, v.stride()),
+                table is None or (table.shape, table.is_contiguous()),
+                length is None or (length.shape, length.is_contiguous()),
+                ks is None or (ks.shape, ks.is_contiguous()), vs is None or (vs.shape, vs.is_contiguous()))
         c = self.__dict__.get("_c")
         if c is None or self._laid != laid:
             self.check()
-            n_seq, max_pages = laid[2] or (0, 0)
+            n_seq, max_pages = (0, 0) if table is None else table.shape
             c = _Cache(None, None, None, None, None, None, *laid[1][:3], *laid[0][:2], n_seq, max_pages, *laid[0][2:],
                        self.dtype, self.weights)
             self.__dict__.update(_laid=laid, _c=c)
-        # The sizes stay while the tensors keep theirs (the struct costs 3 us to build); where memory lies is asked anew.
+        # The sizes stay while all tensors keep theirs (the struct costs 3 us to build); where memory lies is asked anew.
         c.k = k.data_ptr()
         c.v = None if v is None else v.data_ptr()
         c.k_scale = None if ks is None else ks.data_ptr()
@@ -536,9 +539,10 @@ class PageTables:
 
     def pointers(self, n_seq: int, rows: int, dev: int, device) -> list:
         """Where the seven tensors lie.  Their types and layout are checked once for a batch's sizes, and again if a
-        tensor is replaced or resized."""
+        tensor is replaced, resized or laid out otherwise."""
         checked = self.__dict__.get("_checked")
-        if checked is None or checked[0] != (n_seq, rows, dev) or tuple(map(_numel, checked[1])) != checked[2]:
+        if (checked is None or checked[0] != (n_seq, rows, dev) or tuple(map(_numel, checked[1])) != checked[2]
+                or not all(map(_is_contiguous, checked[1]))):
             names = ("seq_len", "q_start", "page_start", "q_seq", "q_pos", "slots", "key_rows")[:6 + (self.key_rows is not None)]
             sizes = (n_seq, n_seq + 1, n_seq + 1, rows, rows, rows, rows)[:len(names)]
             tensors = tuple(_need(getattr(self, name), name, _I32, (n,), device) for name, n in zip(names, sizes))

@@ -297,3 +297,52 @@ def test_unknown_weights_are_refused(lib, monkeypatch, weights):  # noqa: F811
     c.weights = weights
     with pytest.raises(ValueError, match="weights"):
         c.c()
+
+
+# ---- tensors that change in place behind a descriptor's back
+@pytest.mark.parametrize("change,match", [
+    (lambda c: c.v.resize_(4, 8, 2, 128), "v: shape"),
+    (lambda c: c.v.as_strided_((4, 16, 2, 128), (4096, 128, 2048, 1)), "strides"),
+    (lambda c: c.k.as_strided_((4, 16, 2, 128), (4096, 128, 2048, 1)), "strides"),
+    (lambda c: c.k_scale.resize_(3, 16, 2), "k_scale: shape"),
+    (lambda c: c.v_scale.resize_(4, 16, 1), "v_scale: shape"),
+    (lambda c: c.k_scale.as_strided_((4, 16, 2), (32, 1, 16)), "k_scale: not contiguous"),
+    (lambda c: c.seq_len.resize_(2), "seq_len: shape"),
+    (lambda c: c.seq_len.as_strided_((3,), (0,)), "seq_len: not contiguous"),
+    (lambda c: c.block_table.t_(), "block_table: not contiguous"),
+    (lambda c: c.block_table.resize_(2, 3), "seq_len: shape")])
+def test_a_change_in_place_of_any_tensor_is_seen(monkeypatch, change, match):
+    monkeypatch.setattr(hisa, "_on_gpu", lambda t: True)
+    k = torch.zeros((4, 16, 2, 128), dtype=torch.uint8)
+    cache = hisa.Cache(k=k, v=k.clone(), dtype=FP8, block_table=torch.zeros((3, 3), dtype=torch.int32),
+                       seq_len=torch.zeros(3, dtype=torch.int32), k_scale=torch.ones((4, 16, 2)),
+                       v_scale=torch.ones((4, 16, 2)))
+    c = cache.c()
+    assert cache.c() is c and [c.k, c.v, c.k_scale, c.v_scale, c.block_table, c.seq_len] == [
+        t.data_ptr() for t in (cache.k, cache.v, cache.k_scale, cache.v_scale, cache.block_table, cache.seq_len)]
+    change(cache)
+    for _ in range(2):
+        with pytest.raises(ValueError, match=match):
+            cache.c()
+
+
+def test_a_cache_of_keys_alone_and_its_copies(monkeypatch):
+    monkeypatch.setattr(hisa, "_on_gpu", lambda t: True)
+    cache = hisa.Cache(k=torch.zeros((4, 16, 2, 128)), v=None, dtype=F32)
+    c = cache.c()
+    assert c.k == cache.k.data_ptr() and [c.v, c.k_scale, c.v_scale, c.block_table, c.seq_len] == [None] * 5
+    other = copy.copy(cache)
+    cache.k = torch.zeros((4, 8, 2, 128))
+    assert cache.c().page == 8 and other.c().page == 16 and other.c() is not cache.c()
+    cache.v = torch.zeros((4, 8, 2, 128))
+    assert cache.c().v == cache.v.data_ptr() and cache.c().seq_len is None
+
+
+def test_tables_whose_layout_changes_in_place_are_refused(monkeypatch):
+    monkeypatch.setattr(hisa, "_on_gpu", lambda t: True)
+    t = hisa.PageTables.empty(3, 5, "cpu", key_rows=True)
+    device = torch.device("cpu")
+    assert t.pointers(3, 5, -1, device) == t.pointers(3, 5, -1, device)
+    t.q_pos.as_strided_((5,), (0,))
+    with pytest.raises(ValueError, match="q_pos: not contiguous"):
+        t.pointers(3, 5, -1, device)
