@@ -348,7 +348,8 @@ int hisa_cache_append(const hisa_cache* cache, const int32_t* slots, const void*
  * Scores, the running maximum and sum and the output are held in fp32; for the second product (bf16 and
  * fp8 caches) the weights p_s are rounded as cache->weights says.  All sums have a fixed order: the same
  * call gives the same bits.
- * Workspace: hisa_attention_workspace_bytes(queries, cache, 0), which depends on shapes only.
+ * Workspace: hisa_attention_workspace_bytes(queries, cache, 0), which depends on shapes and types only and
+ * not always grows with T.
  */
 int hisa_paged_attention(const hisa_queries* queries, const hisa_cache* cache, const int32_t* q_start,
                          float scale, void* out, float* lse, void* ws, size_t ws_bytes, void* stream);
@@ -368,8 +369,12 @@ int hisa_sparse_attention(const hisa_queries* queries, const hisa_cache* cache, 
                           int32_t k, float scale, void* out, float* lse, void* ws, size_t ws_bytes,
                           void* stream);
 
-/* Workspace in bytes for hisa_paged_attention (k == 0) or hisa_sparse_attention (k >= 1) at these
- * shapes; 0 if none is needed or the shapes are invalid. */
+/* Workspace in bytes for hisa_paged_attention (k == 0) or hisa_sparse_attention (k >= 1) at these shapes and
+ * types; 0 if none is needed or the call would refuse the descriptors.  They are checked as the call checks them, so
+ * the pointers have to be there and aligned; they are not read, and any aligned address gives the size before
+ * the arrays exist.  More queries do not always need more: with enough of them the keys are not split (H = 64, H_kv = 8,
+ * d = 128, one sequence of up to 131072: 34078720 bytes at T = 64 and at T = 256, none at T = 1024).  A workspace for batches
+ * of several sizes is the largest of what each of them asks for. */
 size_t hisa_attention_workspace_bytes(const hisa_queries* queries, const hisa_cache* cache, int32_t k);
 
 /*

@@ -623,7 +623,8 @@ def hisa_cache_append(cache: Cache, slots: torch.Tensor, k_new: torch.Tensor, v_
 
 
 def hisa_attention_workspace_bytes(queries: Queries, cache: Cache, k: int = 0) -> int:
-    """Workspace of hisa_paged_attention (k == 0) or hisa_sparse_attention (k positions per query)."""
+    """Workspace of hisa_paged_attention (k == 0) or hisa_sparse_attention (k positions per query).  A smaller batch may
+    need more than a larger one: a program with several sizes takes the largest of their answers."""
     qc, cc = queries.c(), cache.c()
     return int(lib().hisa_attention_workspace_bytes(C.byref(qc), C.byref(cc), k))
 

@@ -346,3 +346,23 @@ def test_tables_whose_layout_changes_in_place_are_refused(monkeypatch):
     t.q_pos.as_strided_((5,), (0,))
     with pytest.raises(ValueError, match="q_pos: not contiguous"):
         t.pointers(3, 5, -1, device)
+
+
+# ---- workspaces
+def test_a_workspace_is_sized_by_shapes_alone_and_for_each_batch_size(lib):  # noqa: F811
+    def need(T, k=0, at=F, **kw):
+        q, c = queries(T=T, H=64, q=at), cache(max_pages=2048, n_seq=1, H_kv=8, token_stride=1024, page_stride=65536, k=at,
+                                               v=at, block_table=at, seq_len=at, **kw)
+        return lib.hisa_attention_workspace_bytes(C.byref(q), C.byref(c), k)
+
+    # (as the header says)
+    assert [need(T) for T in (64, 256, 1024)] == [34078720, 34078720, 0]
+    for T in (1, 2, 3, 17, 64, 65, 255, 256, 300, 1023, 1024, 4096):
+        for k in (0, 1, 100, 2048, 65536):
+            for kw in (dict(), dict(dtype=FP8), dict(weights=hisa.HISA_WEIGHTS_8BIT)):
+                size = need(T, k, **kw)
+                assert size == need(T, k, at=1 << 40, **kw)             # (whatever the addresses are)
+                q, c = queries(T=T, H=64), cache(max_pages=2048, n_seq=1, H_kv=8, token_stride=1024, page_stride=65536, **kw)
+                if size:                                                # what is a byte less is refused, before any launch
+                    status = paged(lib, q, c, n=size - 1) if k == 0 else sparse(lib, q, c, k=k, n=size - 1)
+                    assert status == WS
