@@ -343,7 +343,7 @@ int hisa_cache_append(const hisa_cache* cache, const int32_t* slots, const void*
  * Supported: q BF16 with a BF16 or FP8_E4M3 cache, d in {64, 128}; q F32 with an F32 cache, d % 4 == 0,
  * d <= 256.  H <= 256, H_kv divides H; page a power of two; k, v and q 16-byte aligned, strides times
  * the element size multiples of 16 bytes; max_pages * page and n_pages * page below 2^31;
- * scale positive and finite.  A launch holds fewer than 2^23 workgroups: split larger calls.  What always
+ * scale positive and finite (below 2^127).  A launch holds fewer than 2^23 workgroups: split larger calls.  What always
  * fits: T * H_kv * ceil(H / H_kv / 32) below that (lists), T * H / 32 + 4 * n_seq * H_kv (ranges).
  * Scores, the running maximum and sum and the output are held in fp32; for the second product (bf16 and
  * fp8 caches) the weights p_s are rounded as cache->weights says.  All sums have a fixed order: the same

@@ -17,6 +17,7 @@ namespace {
 
 constexpr int kMaxHeads = 256, kMaxList = 65536, kMaxAppendD = 512;
 
+constexpr float kLog2e = 1.44269504088896341f;
 constexpr long kMaxThreads = (1L << 32) - 1;   // of a launch: the packet counts them in 32 bits
 
 inline int elem_bytes(int dtype) { return dtype == HISA_F32 ? 4 : dtype == HISA_BF16 ? 2 : 1; }
@@ -147,7 +148,7 @@ AttnArgs attention_args(const hisa_queries* q, const hisa_cache* c, float scale,
   a.page_stride = c->page_stride;
   a.token_stride = c->token_stride;
   a.head_stride = c->head_stride;
-  a.scale_log2 = scale * 1.44269504088896341f;
+  a.scale_log2 = scale * kLog2e;
   a.T = q->T;
   a.H = q->H;
   a.H_kv = c->H_kv;
@@ -232,7 +233,7 @@ int attention(const hisa_queries* q, const hisa_cache* c, const int32_t* q_start
   if (st) return st;
   if (!out || (k ? !list : !q_start)) return HISA_ERR_NULL;
   if (!aligned16(out)) return HISA_ERR_ALIGN;
-  if (!(scale > 0.f) || !std::isfinite(scale)) return HISA_ERR_SHAPE;
+  if (!(scale > 0.f) || !std::isfinite(scale * kLog2e)) return HISA_ERR_SHAPE;
   const AttnPlan p = plan_attention(q, c, k);
   if (p.ws_bytes && (!ws || ws_bytes < p.ws_bytes)) return HISA_ERR_WORKSPACE;
   if (p.ws_bytes && !aligned16(ws)) return HISA_ERR_ALIGN;

@@ -366,3 +366,12 @@ def test_a_workspace_is_sized_by_shapes_alone_and_for_each_batch_size(lib):  # n
                 if size:                                                # what is a byte less is refused, before any launch
                     status = paged(lib, q, c, n=size - 1) if k == 0 else sparse(lib, q, c, k=k, n=size - 1)
                     assert status == WS
+
+
+def test_scales_that_overflow_are_refused(lib):  # noqa: F811
+    """(In units of log2 a scale is 1.44 times as large.)"""
+    q, c = queries(), cache()
+    for scale in (2.4e38, 3.4e38, 2.0 ** 128):
+        assert paged(lib, q, c, scale=scale) == SHAPE and sparse(lib, q, c, scale=scale) == SHAPE
+    # the largest that header allows passes this check (and fails a later one: there is no workspace)
+    assert paged(lib, q, cache(max_pages=2048), scale=1.7e38, ws=None, n=0) == WS
