@@ -1060,14 +1060,17 @@ struct ChunkGeom {
   static constexpr int kLds = kRings + 8 * kChunkKeys * 16 + 8 * 8 + 8 * 4 + (KDT == 2 ? 8 * 2 * kChunkKeys * 4 : 0);
 };
 
-// 16 or 4 bytes per lane from `src` to LDS byte lds + 16 (or 4) * lane.
+// 16 or 4 bytes per lane from `src` to LDS byte lds + 16 (or 4) * lane.  m0 is the compiler's, which takes no clobber of it:
+// it gets back what was there.
 __device__ __forceinline__ void dma16(uint32_t lds, const void* src) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::
-               "s"(__builtin_amdgcn_readfirstlane((int)lds)), "v"(src) : "m0", "memory");
+  int was;
+  asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, off\n\ts_mov_b32 m0, %0" :
+               "=&s"(was) : "s"(__builtin_amdgcn_readfirstlane((int)lds)), "v"(src) : "memory");
 }
 __device__ __forceinline__ void dma4(uint32_t lds, const void* src) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::
-               "s"(__builtin_amdgcn_readfirstlane((int)lds)), "v"(src) : "m0", "memory");
+  int was;
+  asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %2, off\n\ts_mov_b32 m0, %0" :
+               "=&s"(was) : "s"(__builtin_amdgcn_readfirstlane((int)lds)), "v"(src) : "memory");
 }
 template <int N>
 __device__ __forceinline__ void dma_left() {   // until at most N requests of this wave are under way

@@ -14,14 +14,18 @@ def statements():
             yield os.path.basename(path), m.group(0)
 
 
-def test_assembly_names_the_special_registers_that_it_writes():
-    """m0, vcc, exec and scc are the compiler's too: what an instruction's first operand writes has to be among the clobbers."""
+def test_assembly_leaves_the_special_registers_as_they_were():
+    """m0, vcc, exec and scc are the compiler's too.  vcc and scc may be named as clobbers; m0 and exec are reserved, which
+    clobbers do not cover: what writes them saves them first and puts them back at its end."""
     found, wrote = 0, 0
     for path, text in statements():
         found += 1
         strings = re.findall(r'"((?:[^"\\]|\\.)*)"', text)
+        lines = [x.strip() for x in re.split(r"(?:\\n|\\t|;)+", strings[0]) if x.strip()]
         for reg in ("m0", "vcc", "exec", "scc"):
-            if re.search(rf"(?:^|\\n|\\t|;)\s*[sv]_\w+ {reg}\b", strings[0]):
+            if any(re.match(rf"[sv]_\w+ {reg}\b", x) for x in lines):
                 wrote += 1
-                assert reg in strings[1:], f"{path}: {text}"
+                saved = re.fullmatch(rf"s_mov_b(?:32|64) (%\d), {reg}", lines[0])
+                restored = saved and re.fullmatch(rf"s_mov_b(?:32|64) {reg}, {saved.group(1)}", lines[-1])
+                assert restored or reg in ("vcc", "scc") and reg in strings[1:], f"{path}: {text}"
     assert found > 10 and wrote >= 2
