@@ -186,3 +186,21 @@ def test_positions_far_before_the_first_see_nothing(kv, new, far):
     pos[::3] = far
     out, lse = paged.run(b, positions=pos, what=f"position {far}")
     assert (out[::3] == 0).all() and torch.isneginf(lse[::3]).all()
+
+
+@pytest.mark.parametrize("kv", ["bf16", "fp8", "f32"])
+@pytest.mark.parametrize("chunk", [20, 90])
+def test_a_mixed_batch_as_one_call_and_as_calls_of_its_parts(kv, chunk):
+    """Single tokens, idle sequences and a chunk; each part with the same queries and outputs and its share of the tables."""
+    b = Batch([(300 + i, 1) for i in range(9)] + [(0, 0)] * 20 + [(500, chunk)], kv=kv, spare_rows=11, first_row=2, seed=chunk)
+    whole, whole_lse = paged.run(b, what="mixed")
+    b.queries.q_pos = None
+    out, lse = torch.full_like(b.queries.q, 7.25), torch.full((b.T, b.H), 123.0, device=b.dev)
+    for first, last in ((0, 9), (29, 30)):
+        part = hisa.Cache(k=b.cache.k, v=b.cache.v, dtype=b.cache.dtype, k_scale=b.cache.k_scale, v_scale=b.cache.v_scale,
+                          block_table=b.cache.block_table[first:last], seq_len=b.cache.seq_len[first:last])
+        hisa.hisa_paged_attention(b.queries, part, b.q_start[first:last + 1], out=out, lse=lse)
+    torch.cuda.synchronize()
+    mine = b.check(out, lse, b.want(lambda t: np.arange(int(b.pos[t]) + 1)), int(b.seq_len.max()), what="parts", weights=2.0 ** -15)
+    nobody = torch.from_numpy(~mine[:, 0]).to(b.dev)
+    assert (out[nobody] == 7.25).all() and (lse[nobody] == 123.0).all()
