@@ -349,7 +349,7 @@ int hisa_cache_append(const hisa_cache* cache, const int32_t* slots, const void*
  * fp8 caches) the weights p_s are rounded as cache->weights says.  All sums have a fixed order: the same
  * call gives the same bits.
  * How a call is cut up goes by T, n_seq and max_pages, since the lengths are on the device: T <= 2 * n_seq (FP8:
- * 4; n_seq alone where H / H_kv > 32) is taken for a batch of single tokens, each of which reads its keys by itself.  So
+ * 4 * n_seq) is taken for a batch of single tokens, each of which reads its keys by itself.  So
  * pass no idle sequences, little padding and a table of the width in use, and give a long chunk beside single tokens a
  * call of its own: the same queries and out, and the sequence's part of block_table, seq_len (n_seq = 1) and q_start.
  * Workspace: hisa_attention_workspace_bytes(queries, cache, 0), which depends on shapes and types only and

@@ -101,15 +101,16 @@ AttnPlan plan_attention(const hisa_queries* q, const hisa_cache* c, int32_t k) {
   p.rest = c->weights == HISA_WEIGHTS_16BIT;
   // A few new tokens a sequence: one at a time reads their keys that many times, from L2 for the most part, with every
   // wave on keys of its own; together they read them once, but 32 rows are one wave's, and a tile of 64 keys takes it
-  // 4000 cycles from scores to values.  Measured, 64 sequences of 3000, 2 new tokens each: 145 us one at a time, 200
-  // together; 32 of 8000, 4 each: 290 and 323, fp8 220 and 420; 6 each: 354 and 340.  Wide groups fill the tile: 64 heads
-  // on one KV head, 64 sequences of 8000, 2 each: 119 and 97.
+  // 4000 cycles from scores to values.  Measured (one at a time, together), 64 sequences of 3000, 2 new tokens each: 167 and
+  // 210 us, 4 each: 260 and 221, fp8 267 and 262; 32 of 8000, 2 each: 221 and 268, 4 each: 345 and 275, fp8 355 and 325; 64 heads on
+  // one KV head, 64 sequences of 8000, 2 each: 89 and 152, fp8 4 each: 142 and 228; 200 of 500, 32 heads on 8, fp8, 4 each:
+  // 173 and 186.
   // (The lengths are not known here, T counts padding and n_seq idle rows of the table: a chunk in a batch that is as large as
   // this is read token by token too, as often as it has tokens.  64 sequences of 8000 and one chunk of 64 of as many: 527 us,
   // in two calls 422; fp8 and a chunk of 192: 724 and 352; a table of 256 idle rows and a chunk of 512 behind 64K: 8.2 ms, with its
   // own row alone 1.4; fp8 and 1024: 17.4 and 3.1.  And a batch of single tokens padded to more rows takes the chunk kernel: 32
   // of 1000 32 us, in 256 rows 42; fp8 28 and 49.)
-  const long few = G > 32 ? 1 : c->dtype == HISA_FP8_E4M3 ? 4 : 2;
+  const long few = c->dtype == HISA_FP8_E4M3 ? 4 : 2;
   if (c->dtype == HISA_F32) {
     p.kernel = ATTN_F32;
     p.units = k ? T * ((G + 31) / 32) : T * G / 32 + c->n_seq;
