@@ -334,13 +334,13 @@ int hisa_cache_append(const hisa_cache* cache, const int32_t* slots, const void*
  *               tokens than rows: its q_pos is right there too) and q_lo (NULL: 0) as everywhere.  A document
  *               or sliding-window mask is a q_lo, a prefix that sees itself whole a q_pos beyond the
  *               own position.  w, q_seq and q_pos0 are not read
- *   q_start     [n_seq + 1] first token row of each sequence, ascending (device, in), as
+ *   q_start     [n_seq + 1] first token row of each sequence, ascending, T at most (device, in), as
  *               hisa_page_tables writes it.  Rows before q_start[0] and from q_start[n_seq] on belong to
  *               nobody: their out and lse are left as they were
  *   out         [T, H, d] of q_dtype (device, out)
  *   lse         [T, H] fp32 (device, out) or NULL
  * A block_table entry outside [0, n_pages) holds no key that anybody sees.
- * Supported: q BF16 with a BF16 or FP8_E4M3 cache, d in {64, 128}; q F32 with an F32 cache, d % 4 == 0,
+ * Supported: 1 <= T <= 4194304; q BF16 with a BF16 or FP8_E4M3 cache, d in {64, 128}; q F32 with an F32 cache, d % 4 == 0,
  * d <= 256.  H <= 256, H_kv divides H; page a power of two; k, v and q 16-byte aligned, strides times
  * the element size multiples of 16 bytes; max_pages * page and n_pages * page below 2^31;
  * scale positive and finite (below 2^127).  A launch holds fewer than 2^23 workgroups: split larger calls.  What always
@@ -359,8 +359,9 @@ int hisa_paged_attention(const hisa_queries* queries, const hisa_cache* cache, c
                          float scale, void* out, float* lse, void* ws, size_t ws_bytes, void* stream);
 
 /*
- * The same attention over a list of positions per query: what Sparse MLA's sparse attention does with
- * the indexer's output.  Query t of sequence q_seq[t] (NULL: 0) attends to the positions topk_idx[t, :]
+ * The same attention over a list of positions per query, such as the indexer's output, for heads with plain keys and
+ * values of one width d (not over latent rows, whose scores and values have widths of their own: those are refused
+ * as any other d is).  Query t of sequence q_seq[t] (NULL: 0) attends to the positions topk_idx[t, :]
  * (order does not matter; a position named twice counts twice), entries outside [0, seq_len) are
  * skipped, so both hisa_token_refine_topk's lists and hisa_block_sparse_tokens' fit; a query whose
  * sequence is outside [0, n_seq) sees nothing.  Whether a position is visible is the list's business:

@@ -204,3 +204,17 @@ def test_a_mixed_batch_as_one_call_and_as_calls_of_its_parts(kv, chunk):
     mine = b.check(out, lse, b.want(lambda t: np.arange(int(b.pos[t]) + 1)), int(b.seq_len.max()), what="parts", weights=2.0 ** -15)
     nobody = torch.from_numpy(~mine[:, 0]).to(b.dev)
     assert (out[nobody] == 7.25).all() and (lse[nobody] == 123.0).all()
+
+
+@pytest.mark.parametrize("kv", ["bf16", "fp8", "f32"])
+def test_tokens_beyond_the_rows_with_the_tables_positions(kv):
+    """More new tokens than rows: the rows there are stand for the first of them, which the tables' q_pos says."""
+    b = Batch([(40, 30), (10, 125)], kv=kv, seed=3)
+    rows = 70
+    t = hisa.hisa_page_tables(b.put([40, 10]), b.put([30, 125]), b.cache.block_table.clone(), b.page, b.put(range(20)), rows)
+    assert t.q_start.tolist() == [0, 30, 70] and torch.equal(t.seq_len, b.cache.seq_len)
+    b.T, b.starts, b.q_start = rows, np.array([0, 30, 70], np.int32), t.q_start
+    b.q64, b.q_seq, b.pos = b.q64[:rows], b.q_seq[:rows], b.pos[:rows]
+    assert t.q_pos.tolist() == b.pos.tolist()
+    b.queries = hisa.Queries(q=b.queries.q[:rows].contiguous(), w=None, dtype=b.queries.dtype)
+    paged.run(b, positions=t.q_pos.cpu().numpy(), what="cut short")
