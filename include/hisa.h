@@ -247,7 +247,7 @@ int hisa_index_iou(const int32_t* a_idx, const int32_t* b_idx, int32_t T, int32_
  *   HISA_WEIGHTS_16BIT  (0) two bf16 parts of each weight, 16 bits together: a result is off by little more than its
  *                       own rounding to bf16
  *   HISA_WEIGHTS_8BIT   one bf16, 8 bits: a result of many keys is off by up to 1.45 times that in the mean square.
- *                       For prompts, where the second part costs a fifth to a third of the call; single tokens wait
+ *                       For prompts, where the second part is a sixth to a quarter of the call; single tokens wait
  *                       for memory and gain nothing
  */
 typedef enum { HISA_WEIGHTS_16BIT = 0, HISA_WEIGHTS_8BIT = 1 } hisa_weights;

@@ -118,8 +118,8 @@ AttnPlan plan_attention(const hisa_queries* q, const hisa_cache* c, int32_t k) {
     splits = parts(p.units * c->H_kv, (c->d > 128 ? 1 : 2) * kCus, keys, most, !k);
   } else if (k || T <= few * c->n_seq) {
     p.kernel = ATTN_ROWS;
-    // (one gathering of the keys for up to 64 heads: lists of 2048, 64 heads on one KV head, 1024 queries 155 us, two
-    // workgroups of 32 heads each 212)
+    // (one gathering of the keys for up to 64 heads: lists of 2048, 64 heads on one KV head, 1024 queries 159 us, two
+    // workgroups of 32 heads each 221; 32 queries 20.9 and 19.2)
     p.pair = G > 32;
     const long heads = p.pair ? 64 : 32;
     p.units = T * ((G + heads - 1) / heads);
