@@ -346,7 +346,8 @@ int hisa_cache_append(const hisa_cache* cache, const int32_t* slots, const void*
  * scale positive and finite (below 2^127).  A launch holds fewer than 2^23 workgroups: split larger calls.  What always
  * fits: T * H_kv * ceil(H / H_kv / 32) below that (lists), T * H / 32 + 4 * n_seq * H_kv (ranges).
  * Scores, the running maximum and sum and the output are held in fp32; for the second product (bf16 and
- * fp8 caches) the weights p_s are rounded as cache->weights says.  All sums have a fixed order: the same
+ * fp8 caches) the weights p_s are rounded as cache->weights says.  Weights are kept below 2^8 until the division by their
+ * sum, so finite values (scale * code) of 2^88 and less never overflow, whatever their number.  All sums have a fixed order: the same
  * call gives the same bits.
  * How a call is cut up goes by T, n_seq and max_pages, since the lengths are on the device: T <= 2 * n_seq (FP8:
  * 4 * n_seq) is taken for a batch of single tokens, each of which reads its keys by itself.  So
